@@ -276,9 +276,10 @@ int fvar_cache_len(const fvar_ctx *ctx, int block);
 long long fvar_launch_count(const fvar_ctx *ctx);
 
 /* Synchronises the stream, reads the device status word and clears it.  FVAR_OK, FVAR_ETIMEOUT,
- * FVAR_EINVAL (bad forced_indices) or FVAR_ECUDA.  After a timeout the results of the steps since the last
- * poll are invalid; the library clears its reduction counters and drops its captured graphs, and the context
- * can be used again.  ctx == NULL polls the status word of the kernel-level entry points on the current device. */
+ * FVAR_EINVAL (bad forced_indices; with ctx == NULL a start of fvar_kv4_write or fvar_kv4_read outside the cache) or
+ * FVAR_ECUDA.  After a timeout the results of the steps since the last poll are invalid; the library clears its reduction
+ * counters and drops its captured graphs, and the context can be used again.  ctx == NULL polls the status word of the
+ * kernel-level entry points on the current device. */
 fvar_status fvar_poll_status(fvar_ctx *ctx);
 
 /* Empties the KV cache and the group caches (host state only; device memory is not cleared). */
@@ -378,6 +379,49 @@ fvar_status fvar_gemm_bf16_form(const void *A, const void *W, const void *bias, 
  * transposed); out dev bf16 [B][r][H*D].  D in {64, 128}; L_cap % 8 == 0; 1 <= L <= L_cap. */
 fvar_status fvar_attention(const void *q, const void *Kc, const void *Vt, int B, int H, int r, int D, int L,
                            int L_cap, void *out, void *stream);
+
+/* ---- A cache of keys and values in 4 bits a value (the paper has no counterpart; its cache is bf16) ------------
+ * A row of a head has head_dim values in groups of 32.  Each group has a scale s = (1 + m / 8) 2^(e - 20), kept as the byte
+ * 8 e + m (e in 0..31, m in 0..7), and 32 numbers u of 4 bits; a value is (u - 8) s.  Eight values are a 32-bit little-endian
+ * word: value 2 p at bits 4 p .. 4 p + 3, value 2 p + 1 at bits 16 + 4 p ..  4.25 bits a value, and every value is exact in
+ * bf16.  Quantising takes the least scale with 7.5 s >= max |x| of the group (byte 0 for a group of zeros, byte 255 = 3840
+ * beyond it) and u - 8 = sign(x) min(7, floor(|x| / s + 1/2)): off by at most s / 2 up to |x| = 28800.  A NaN becomes 0 and
+ * does not count in the maximum; infinities take 7 at the greatest scale, which leaves 0 of small values beside them.
+ *   k_codes, v_codes    dev [B][n_heads][L_cap][head_dim / 2] bytes
+ *   k_scales, v_scales  dev [B][n_heads][L_cap][head_dim / 32] bytes, all four 16-byte aligned
+ *   elem_stride         cache rows from one element to the next, a multiple of 8, at least n_heads * L_cap (0: that): with
+ *                       2 n_heads L_cap and pointers at element 1 the cache holds the null-prompt elements of CFG pairs
+ * head_dim in {64, 128}; L_cap % 8 == 0.  What lies in rows that nobody wrote is never used. */
+typedef struct {
+  void *k_codes, *v_codes, *k_scales, *v_scales;
+  int B, n_heads, head_dim, L_cap;
+  long long elem_stride;
+} fvar_kv4;
+
+/* Quantises rows as they are written: row i < count[b] of element b goes to cache row L0 + i, or start[b] + i.
+ * K, V dev bf16, row (b, i) at (b * n + i) * ld elements, n_heads * head_dim long (ld % 8 == 0, ld >= that: rows may be
+ * columns of a wider matrix, such as the keys and values of a fused QKV product); 16-byte aligned.  start dev int32 [B] or
+ * NULL (then L0 for every element); count dev int32 [B] or NULL (then n; values beyond [0, n] count as its ends).
+ * Rows that would fall outside the cache are not written; with L0 that is FVAR_EINVAL, with start the next
+ * fvar_poll_status(NULL) returns FVAR_EINVAL.  n == 0 does nothing. */
+fvar_status fvar_kv4_write(const fvar_kv4 *cache, const void *K, const void *V, long long ld, int n, int L0, const int *start,
+                           const int *count, void *stream);
+
+/* Reads rows back: K_out, V_out dev bf16 [B][n][n_heads * head_dim], 16-byte aligned; start and count as above.  Rows of the
+ * outputs at or beyond count[b], and those that would come from outside the cache, are left as they were.  The result has
+ * the layout that fvar_load_kv takes (one block's part of it). */
+fvar_status fvar_kv4_read(const fvar_kv4 *cache, int n, int L0, const int *start, const int *count, void *K_out, void *V_out,
+                          void *stream);
+
+/* softmax(q k^T / sqrt(D)) v per head over a cache in 4 bits: fvar_attention on the values the cache stands for.
+ * q dev bf16, row (b, i) at (b * r + i) * ldq elements, H * D long (ldq % 8 == 0); out dev bf16 [B][r][H * D]; both 16-byte
+ * aligned and apart from each other; B and D are the cache's.  H is a multiple of the cache's n_heads; query head h reads
+ * cache head h / (H / n_heads).  Row i of element b sees the first min(L, limits[b][i]) rows of its element (limits dev int32
+ * [B][r], negative ones count as 0; NULL: the first L rows for every query row).  limits express padded batches, causal rows
+ * and the rows of several scales at once, each up to the end of its own scale.  A row that sees nothing becomes 0.
+ * 0 <= L <= L_cap; r >= 1. */
+fvar_status fvar_attention_kv4(const void *q, long long ldq, const fvar_kv4 *cache, int H, int r, int L, const int *limits, void *out,
+                               void *stream);
 
 /* Failure-detection self-test: launches one CTA that waits, with a budget of `cycles` clock cycles, on a
  * barrier nothing ever signals.  The wait gives up, the kernel records FVAR_ETIMEOUT in the status word and

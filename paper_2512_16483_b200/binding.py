@@ -55,6 +55,11 @@ class _Policy(ct.Structure):
                 ("sample_noise", ct.c_void_p), ("restore", ct.c_int)]
 
 
+class _Kv4(ct.Structure):
+    _fields_ = [("k_codes", ct.c_void_p), ("v_codes", ct.c_void_p), ("k_scales", ct.c_void_p), ("v_scales", ct.c_void_p),
+                ("B", ct.c_int), ("n_heads", ct.c_int), ("head_dim", ct.c_int), ("L_cap", ct.c_int), ("elem_stride", ct.c_longlong)]
+
+
 _lib = None
 _calls = None                    # the short calls in native code (csrc/pycalls.cpp)
 
@@ -110,6 +115,9 @@ def load_library() -> ct.CDLL:
         "fvar_gemm_bf16_form": (i, [vp, vp, vp, i, i, i, i, i, vp, vp]),
         "fvar_gemm_bf16_wt": (i, [vp, vp, vp, i, i, i, i, vp, vp]),
         "fvar_attention": (i, [vp, vp, vp, i, i, i, i, i, i, vp, vp]),
+        "fvar_kv4_write": (i, [P(_Kv4), vp, vp, ll, i, i, vp, vp, vp]),
+        "fvar_kv4_read": (i, [P(_Kv4), i, i, vp, vp, vp, vp, vp]),
+        "fvar_attention_kv4": (i, [vp, ll, P(_Kv4), i, i, i, vp, vp, vp]),
         "fvar_rtr_fill": (i, [vp, i, i, i, i, i, i, vp, vp, vp]),
         "fvar_select_rows_static": (i, [vp, i, i, i, i, vp, vp, vp]),
         "fvar_l2_prefetch": (i, [vp, ct.c_size_t, vp]),
@@ -150,7 +158,7 @@ EXPORTED = ("fvar_workspace_bytes", "fvar_init", "fvar_set_cond", "fvar_set_proj
             "fvar_load_group_cache", "fvar_cache_len", "fvar_launch_count", "fvar_poll_status", "fvar_reset",
             "fvar_destroy", "fvar_last_error", "fvar_restore_loaded", "fvar_set_option", "fvar_profile_enable", "fvar_profile_read", "fvar_profile_dump",
             "fvar_row_scores", "fvar_row_keys", "fvar_select_topr", "fvar_ln_modulate",
-            "fvar_gemm_bf16", "fvar_gemm_bf16_form", "fvar_gemm_bf16_wt", "fvar_cfg_combine", "fvar_attention", "fvar_rtr_fill", "fvar_select_rows_static", "fvar_l2_prefetch", "fvar_selftest_wait_timeout",
+            "fvar_gemm_bf16", "fvar_gemm_bf16_form", "fvar_gemm_bf16_wt", "fvar_cfg_combine", "fvar_attention", "fvar_kv4_write", "fvar_kv4_read", "fvar_attention_kv4", "fvar_rtr_fill", "fvar_select_rows_static", "fvar_l2_prefetch", "fvar_selftest_wait_timeout",
             "fvar_rank_from_keep_ratio", "fvar_rank_from_table_ratio", "fvar_infinity_rank_ratio", "fvar_infinity_group_ranks",
             "fvar_infinity_schedule")
 
@@ -285,6 +293,102 @@ def fvar_attention(q: torch.Tensor, Kc: torch.Tensor, Vt: torch.Tensor, L: int) 
     out = torch.empty_like(q)
     _check_kernel(load_library().fvar_attention(q.data_ptr(), Kc.data_ptr(), Vt.data_ptr(), B, H, r, D, L, L_cap,
                                                 out.data_ptr(), _stream()))
+    return out
+
+
+class Kv4:
+    """A cache of keys and values in 4 bits a value (format: include/fvar.h) over the caller's tensors: codes uint8
+    [B][n_heads][L_cap][D / 2], scales uint8 [B][n_heads][L_cap][D / 32].  Views of some elements ([1::2]: the null-prompt ones
+    of CFG pairs) are caches too."""
+
+    def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor):
+        B, H, L_cap, half = k_codes.shape
+        D = 2 * half
+        stride = None
+        for t, d in ((k_codes, half), (v_codes, half), (k_scales, D // 32), (v_scales, D // 32)):
+            assert t.is_cuda and t.dtype == torch.uint8 and t.device == k_codes.device, (t.device, t.dtype)
+            assert tuple(t.shape) == (B, H, L_cap, d) and t[0].is_contiguous(), (tuple(t.shape), t.stride())
+            rows = t.stride(0) // d if B > 1 else H * L_cap
+            assert stride in (None, rows) and (B == 1 or t.stride(0) == rows * d), "elements are not equally far apart"
+            stride = rows
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales    # kept alive
+        self.B, self.n_heads, self.L_cap, self.head_dim, self.device = B, H, L_cap, D, k_codes.device
+        self._c = _Kv4(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), B, H, D, L_cap, stride)
+        self._ref = ct.byref(self._c)
+
+    @classmethod
+    def empty(cls, B: int, n_heads: int, L_cap: int, head_dim: int) -> "Kv4":
+        """A cache of its own; L_cap is rounded up to a multiple of 8."""
+        shape = (B, n_heads, (L_cap + 7) // 8 * 8)
+        return cls(*(torch.empty(shape + (d,), dtype=torch.uint8, device="cuda") for d in (head_dim // 2, head_dim // 2, head_dim // 32, head_dim // 32)))
+
+    def elements(self, which: slice) -> "Kv4":
+        """The cache of some of the elements; nothing is copied."""
+        return Kv4(self.k_codes[which], self.v_codes[which], self.k_scales[which], self.v_scales[which])
+
+
+def _rows_of(t: torch.Tensor, device) -> int:
+    """Elements from one row of t bf16 [B][n][C] to the next; rows may be columns of a wider matrix."""
+    assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3 and t.device == device, (t.device, t.dtype, tuple(t.shape))
+    B, n, C = t.shape
+    ld = t.stride(1) if n > 1 else t.stride(0) if B > 1 else C
+    assert (t.stride(2) == 1 or C == 1) and (B == 1 or n == 0 or t.stride(0) == n * ld), "rows are not equally far apart"
+    return ld
+
+
+def _kv4_place(cache: Kv4, start, count):
+    """(L0, start, count) of a call as the library takes them."""
+    for t in (start, count):
+        if isinstance(t, torch.Tensor):
+            _dev(t, torch.int32)
+            assert tuple(t.shape) == (cache.B,) and t.device == cache.device, (tuple(t.shape), t.device)
+    return (0, start.data_ptr(), _ptr(count)) if isinstance(start, torch.Tensor) else (int(start), None, _ptr(count))
+
+
+def _current(device):
+    assert device.index == torch.cuda.current_device(), "tensors on %s, current device %d" % (device, torch.cuda.current_device())
+
+
+def fvar_kv4_write(cache: Kv4, K: torch.Tensor, V: torch.Tensor, start, count: Optional[torch.Tensor] = None):
+    """Quantises rows of K, V bf16 [B][n][n_heads * D] into the cache: row i < count[b] to cache row start + i (start an int,
+    or int32 [B]).  K and V may be columns of a wider matrix."""
+    _current(cache.device)
+    ld = _rows_of(K, cache.device)
+    assert K.shape == V.shape and K.shape[0] == cache.B and K.shape[2] == cache.n_heads * cache.head_dim, (tuple(K.shape), tuple(V.shape))
+    assert _rows_of(V, cache.device) == ld, "rows of K and V are not equally far apart"
+    L0, st, cn = _kv4_place(cache, start, count)
+    _check_kernel(load_library().fvar_kv4_write(cache._ref, K.data_ptr(), V.data_ptr(), ld, K.shape[1], L0, st, cn, _stream()))
+
+
+def fvar_kv4_read(cache: Kv4, n: int, start, count: Optional[torch.Tensor] = None, out=None):
+    """Cache rows start .. start + n - 1 as bf16 (K, V), each [B][n][n_heads * D], or into out = (K, V).  Rows at or beyond
+    count[b] are left as they were (zero without out)."""
+    _current(cache.device)
+    L0, st, cn = _kv4_place(cache, start, count)
+    shape = (cache.B, n, cache.n_heads * cache.head_dim)
+    if out is None:
+        make = torch.empty if st is None and cn is None else torch.zeros
+        out = tuple(make(shape, dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+    for t in out:
+        assert tuple(_dev(t, torch.bfloat16).shape) == shape and t.device == cache.device, (tuple(t.shape), shape)
+    _check_kernel(load_library().fvar_kv4_read(cache._ref, n, L0, st, cn, out[0].data_ptr(), out[1].data_ptr(), _stream()))
+    return out
+
+
+def fvar_attention_kv4(q: torch.Tensor, cache: Kv4, L: int, limits: Optional[torch.Tensor] = None,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q bf16 [B][r][H * D] over the first L rows of a cache in 4 bits (row i of element b over the first limits[b][i], int32
+    [B][r]) -> bf16 [B][r][H * D].  H may be a multiple of the cache's heads; q may be columns of a wider matrix."""
+    _current(cache.device)
+    ld = _rows_of(q, cache.device)
+    B, r, C = q.shape
+    assert B == cache.B and C % cache.head_dim == 0, (tuple(q.shape), cache.B, cache.head_dim)
+    if limits is not None:
+        assert tuple(_dev(limits, torch.int32).shape) == (B, r) and limits.device == cache.device, tuple(limits.shape)
+    if out is None:
+        out = torch.empty((B, r, C), dtype=torch.bfloat16, device=q.device)
+    assert tuple(_dev(out, torch.bfloat16).shape) == (B, r, C) and out.device == cache.device, tuple(out.shape)
+    _check_kernel(load_library().fvar_attention_kv4(q.data_ptr(), ld, cache._ref, C // cache.head_dim, r, L, _ptr(limits), out.data_ptr(), _stream()))
     return out
 
 

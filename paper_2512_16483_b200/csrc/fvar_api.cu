@@ -466,6 +466,15 @@ GemmArgs gemm_args(int R, int N, int K) {
   return g;
 }
 
+// The fields of a cache in 4 bits as the kernels take them.
+template <typename A>
+void kv4_fields(const fvar_kv4 *c, A &a) {
+  a.k_codes = static_cast<uint8_t *>(c->k_codes); a.v_codes = static_cast<uint8_t *>(c->v_codes);
+  a.k_scales = static_cast<uint8_t *>(c->k_scales); a.v_scales = static_cast<uint8_t *>(c->v_scales);
+  a.elem_stride = c->elem_stride ? c->elem_stride : static_cast<long long>(c->n_heads) * c->L_cap;
+  a.B = c->B; a.D = c->head_dim; a.L_cap = c->L_cap;
+}
+
 }  // namespace
 
 // ================================================================================================
@@ -799,7 +808,7 @@ fvar_status fvar_poll_status(fvar_ctx *ctx) {
     if (word) FV_CUDA(ctx, cudaMemset(ks, 0, sizeof(word)), "status clear");
   }
   if (word & kStatusTimeout) return fail(ctx, FVAR_ETIMEOUT, "a device-side wait ran out");
-  if (word & kStatusBadIndex) return fail(ctx, FVAR_EINVAL, "forced_indices out of range or not ascending");
+  if (word & kStatusBadIndex) return fail(ctx, FVAR_EINVAL, ctx ? "forced_indices out of range or not ascending" : "rows outside a 4-bit cache");
   return FVAR_OK;
 }
 
@@ -1717,6 +1726,66 @@ fvar_status fvar_attention(const void *q, const void *Kc, const void *Vt, int B,
   attention_plan(B, H, r, L, sms, &a.tiles_per_cta, &a.kv_splits);
   if (!a.status) return kfail(FVAR_ECUDA, "attention: status word");
   FK_CUDA(launch_attention(tq, tk, tv, a, sms, static_cast<cudaStream_t>(stream)), "attention");
+  return FVAR_OK;
+}
+
+// What is wrong with a cache in 4 bits (nullptr: nothing).
+static const char *kv4_wrong(const fvar_kv4 *c) {
+  if (!c || !c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) return "kv4: NULL cache or array";
+  if (c->B <= 0 || c->n_heads <= 0 || c->L_cap <= 0 || c->L_cap % 8 || (c->head_dim != 64 && c->head_dim != 128)) return "kv4: bad shape of the cache";
+  if (c->elem_stride != 0 && (c->elem_stride % 8 || c->elem_stride < static_cast<long long>(c->n_heads) * c->L_cap)) return "kv4: bad element stride";
+  if (off_grid(c->k_codes, 16) || off_grid(c->v_codes, 16) || off_grid(c->k_scales, 16) || off_grid(c->v_scales, 16))
+    return "kv4: the cache's arrays must be 16-byte aligned";
+  return nullptr;
+}
+static fvar_status kv4_rows(bool write, const fvar_kv4 *cache, Kv4Args &a, int n, int L0, const int *start, const int *count, void *stream) {
+  if (n < 0) return kfail(FVAR_EINVAL, "kv4: n must not be negative");
+  if (!start && (L0 < 0 || L0 > cache->L_cap - n)) return kfail(FVAR_EINVAL, "kv4: rows outside the cache");
+  if (n == 0) return FVAR_OK;
+  kv4_fields(cache, a);
+  a.H = cache->n_heads; a.n = n; a.L0 = L0; a.start = start; a.count = count;
+  a.status = kernel_status_ptr();
+  if (!a.status) return kfail(FVAR_ECUDA, "kv4: status word");
+  FK_CUDA(launch_kv4_rows(write, a, static_cast<cudaStream_t>(stream)), write ? "kv4_write" : "kv4_read");
+  return FVAR_OK;
+}
+
+fvar_status fvar_kv4_write(const fvar_kv4 *cache, const void *K, const void *V, long long ld, int n, int L0, const int *start,
+                           const int *count, void *stream) {
+  if (const char *why = kv4_wrong(cache)) return kfail(FVAR_EINVAL, why);
+  if (!K || !V || ld % 8 || ld < static_cast<long long>(cache->n_heads) * cache->head_dim) return kfail(FVAR_EINVAL, "kv4_write: bad rows");
+  if (off_grid(K, 16) || off_grid(V, 16)) return kfail(FVAR_EINVAL, "kv4_write: K and V must be 16-byte aligned");
+  Kv4Args a = {};
+  a.k_rows = static_cast<const bf16 *>(K); a.v_rows = static_cast<const bf16 *>(V); a.ld = ld;
+  return kv4_rows(true, cache, a, n, L0, start, count, stream);
+}
+
+fvar_status fvar_kv4_read(const fvar_kv4 *cache, int n, int L0, const int *start, const int *count, void *K_out, void *V_out, void *stream) {
+  if (const char *why = kv4_wrong(cache)) return kfail(FVAR_EINVAL, why);
+  if (!K_out || !V_out) return kfail(FVAR_EINVAL, "kv4_read: NULL output");
+  if (off_grid(K_out, 16) || off_grid(V_out, 16)) return kfail(FVAR_EINVAL, "kv4_read: K_out and V_out must be 16-byte aligned");
+  Kv4Args a = {};
+  a.k_out = static_cast<bf16 *>(K_out); a.v_out = static_cast<bf16 *>(V_out);
+  return kv4_rows(false, cache, a, n, L0, start, count, stream);
+}
+
+fvar_status fvar_attention_kv4(const void *q, long long ldq, const fvar_kv4 *cache, int H, int r, int L, const int *limits, void *out,
+                               void *stream) {
+  if (const char *why = kv4_wrong(cache)) return kfail(FVAR_EINVAL, why);
+  if (!q || !out || H <= 0 || H % cache->n_heads || r <= 0 || L < 0 || L > cache->L_cap || ldq % 8 || ldq < static_cast<long long>(H) * cache->head_dim)
+    return kfail(FVAR_EINVAL, "attention_kv4: bad arguments");
+  if (off_grid(q, 16) || off_grid(out, 16)) return kfail(FVAR_EINVAL, "attention_kv4: q and out must be 16-byte aligned");
+  Kv4AttnArgs a = {};
+  kv4_fields(cache, a);
+  a.q = static_cast<const bf16 *>(q); a.ldq = ldq; a.H = H; a.Hkv = cache->n_heads; a.r = r; a.L = L; a.limits = limits;
+  a.out = static_cast<bf16 *>(out);
+  a.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(a.D));
+  a.status = kernel_status_ptr();
+  if (!a.status) return kfail(FVAR_ECUDA, "attention_kv4: status word");
+  int dev = 0, sms = 0;
+  FK_CUDA(cudaGetDevice(&dev), "get device");
+  FK_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev), "device attribute");
+  FK_CUDA(launch_attention_kv4(a, sms, static_cast<cudaStream_t>(stream)), "attention_kv4");
   return FVAR_OK;
 }
 

@@ -294,6 +294,30 @@ cudaError_t launch_chol_inverse(const float *G, float *Ginv, int r, int count, u
 cudaError_t launch_split_rows(const float *x, long long x_off, long long x_stride, int E, int M, int C, bf16 *xsplit, int mk,
                               cudaStream_t st);
 
+// Cache in 4 bits (kv4.cu, attention_kv4.cu; format in include/fvar.h).
+struct Kv4Args {
+  const bf16 *k_rows, *v_rows;            // write: row (b, i) at (b * n + i) * ld
+  bf16 *k_out, *v_out;                    // read: [B][n][H * D]
+  uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
+  long long ld, elem_stride;              // elem_stride: cache rows from one element to the next
+  int B, H, D, L_cap, n, L0;
+  const int *start, *count;
+  unsigned *status;
+  long long units;                        // warps' work, filled by launch_kv4_rows
+};
+cudaError_t launch_kv4_rows(bool write, Kv4Args a, cudaStream_t st);
+struct Kv4AttnArgs {
+  const bf16 *q;
+  const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
+  long long ldq, elem_stride;
+  int B, H, Hkv, r, D, L, L_cap;
+  const int *limits;                      // [B][r] or nullptr
+  bf16 *out;                              // [B][r][H * D]
+  float scale_log2;                       // log2(e) / sqrt(D)
+  unsigned *status;
+};
+cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, int num_sms, cudaStream_t st);
+
 // Self-test of the bounded wait: one CTA waits on an mbarrier nobody signals with a budget of `cycles`, flags the
 // status word and returns.
 cudaError_t launch_wait_selftest(long long cycles, unsigned *status, cudaStream_t st);
