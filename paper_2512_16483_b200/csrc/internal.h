@@ -315,6 +315,8 @@ struct Kv4AttnArgs {
   bf16 *out;                              // [B][r][H * D]
   float scale_log2;                       // log2(e) / sqrt(D)
   unsigned *status;
+  long long wait_cycles;                  // budget of every bounded wait (0: the default)
+  int kv_splits;                          // ranges of keys, a cluster's CTAs; filled by launch_attention_kv4
 };
 cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, int num_sms, cudaStream_t st);
 
