@@ -36,6 +36,11 @@ __device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
   asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
   return v;
 }
+__device__ __forceinline__ unsigned add_acq_rel(uint32_t addr, unsigned v) {
+  unsigned old;
+  asm volatile("atom.acq_rel.cta.shared::cta.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(addr), "r"(v) : "memory");
+  return old;
+}
 template <int N>
 __device__ __forceinline__ void ld_shared_words(uint32_t addr, uint32_t (&w)[N]) {
   if constexpr (N == 4) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr));
@@ -43,19 +48,18 @@ __device__ __forceinline__ void ld_shared_words(uint32_t addr, uint32_t (&w)[N])
   if constexpr (N == 1) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(addr));
 }
 
-// What a query row's share of a range of keys adds: a range without any key has m = -inf and l = 0 and weighs nothing.
-__device__ __forceinline__ float range_weight(float m, float l, float m_all) { return l == 0.f ? 0.f : exp2f(m - m_all); }
+// Running maxima start here: finite, so that no difference of two of them is a NaN.
+constexpr float kNoMax = -3.0e38f;
+// What a query row's share of a range of keys weighs; m in units of the scores, c of log2.  A range without any key has l = 0.
+__device__ __forceinline__ float range_weight(float m, float l, float m_all, float c) { return l == 0.f ? 0.f : exp2f((m - m_all) * c); }
 
-constexpr int kFewWarps = 8;                              // that compute; one more requests the tiles
-constexpr int kFewThreads = 32 * (kFewWarps + 1);
-constexpr int kFewKeys = 16 * kFewWarps;                  // keys of one round of the warps
-constexpr int kFewRounds = 2;                             // rounds a stage
-constexpr int kFewStageKeys = kFewKeys * kFewRounds;
+constexpr int kFewSets = 2;                               // sets of 16 keys that a warp takes of a stage
 constexpr int kFewStages = 3;
 constexpr int kFewMaxRanges = 8;
 
-template <int D, int NB>
+template <int D, int NB, int W>
 struct FewCfg {
+  static constexpr int kFewWarps = W, kFewThreads = 32 * W, kFewKeys = 16 * W, kFewStageKeys = kFewKeys * kFewSets;
   static constexpr int kRows = 8 * NB;                    // query rows of a unit
   static constexpr int kCodeBytes = kFewStageKeys * D / 2, kScaleBytes = kFewStageKeys * D / kKv4Group;
   static constexpr int kStageBytes = 2 * (kCodeBytes + kScaleBytes);          // K codes, V codes, K scales, V scales
@@ -64,21 +68,23 @@ struct FewCfg {
   static constexpr int kQuads = kRows * D / 4;            // float4 of a unit
   static constexpr int kRecvBytes = (kQuads + kFewMaxRanges) * 16;            // what the ranges of a cluster push here
   static constexpr int kMlBytes = kFewMaxRanges * kRows * 8;
-  static constexpr int kSmemBytes = kFewStages * kStageBytes + kRecvBytes + kMlBytes + 128;
-  static_assert(kPartBytes + kFewWarps * kRows * 8 <= kFewStages * kStageBytes, "parts");
+  static constexpr int kStagesBytes = kFewStages * kStageBytes, kAllParts = (kPartBytes + kFewWarps * kRows * 8 + 127) / 128 * 128;
+  static constexpr int kFrontBytes = kStagesBytes > kAllParts ? kStagesBytes : kAllParts;
+  static constexpr int kSmemBytes = kFrontBytes + kRecvBytes + kMlBytes + 128;
 };
 
-template <int D, int NB>
-__global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_few_kernel(const __grid_constant__ Kv4AttnArgs p) {
-  using Cfg = FewCfg<D, NB>;
+template <int D, int NB, int W>
+__global__ void __launch_bounds__(32 * W, (NB == 1 ? 16 : 8) / W) attention_kv4_few_kernel(const __grid_constant__ Kv4AttnArgs p) {
+  using Cfg = FewCfg<D, NB, W>;
+  constexpr int kFewWarps = W, kFewThreads = 32 * W, kFewKeys = Cfg::kFewKeys, kFewStageKeys = Cfg::kFewStageKeys;
   constexpr int KW = D / 32, VW = D / 64;                 // words a lane takes of a key row, of a value row
   extern __shared__ __align__(128) uint8_t smem_raw[];
-  __shared__ uint64_t bars[2 * kFewStages];
+  __shared__ uint64_t bars[kFewStages];
+  __shared__ unsigned done[kFewStages];                   // warps that have finished with a slot, in all its uses
   __shared__ volatile int abort_flag;
   const uint32_t stages = smem_u32(smem_raw);
-  const uint32_t recv = stages + kFewStages * Cfg::kStageBytes, recv_ml = recv + Cfg::kRecvBytes;
+  const uint32_t recv = stages + Cfg::kFrontBytes, recv_ml = recv + Cfg::kRecvBytes;
   auto full = [&](int s) { return smem_u32(&bars[s]); };
-  auto empty = [&](int s) { return smem_u32(&bars[kFewStages + s]); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
   const long long wb = wait_budget(p.wait_cycles);
 
@@ -86,7 +92,7 @@ __global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_fe
     abort_flag = 0;
     for (int s = 0; s < kFewStages; ++s) {
       mbar_init(full(s), 1);
-      mbar_init(empty(s), kFewWarps);
+      done[s] = 0;
     }
     mbar_fence_init();
   }
@@ -113,9 +119,11 @@ __global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_fe
   // Its keys, in ranges of whole rounds: [k0, k1) here.
   const int rounds = (kmax + kFewKeys - 1) / kFewKeys, per = (rounds + splits - 1) / splits;
   const int k0 = min(sp * per * kFewKeys, kmax), k1 = min(k0 + per * kFewKeys, kmax);
+  kmin = min(kmin, k1);
   const int nst = (k1 - k0 + kFewStageKeys - 1) / kFewStageKeys;
   const long long row0 = b * p.elem_stride + static_cast<long long>(kv) * p.L_cap;
 
+  const float c = p.scale_log2;
   float o[NB][D / 16][4];
   float m[NB][2], l[NB][2];
 #pragma unroll
@@ -124,33 +132,23 @@ __global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_fe
     for (int t = 0; t < D / 16; ++t)
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[nb][t][k] = 0.f;
-    m[nb][0] = m[nb][1] = -INFINITY;
+    m[nb][0] = m[nb][1] = kNoMax;
     l[nb][0] = l[nb][1] = 0.f;
   }
 
-  if (warp == kFewWarps) {
-    if (lane == 0) {
-      // ---------------------------------------------------------------- requests
-      const int kend = (k1 + 7) & ~7;                     // whole 16 bytes of scales; within the cache (L_cap % 8 == 0)
-      int st = 0;
-      for (; st < nst; ++st) {
-        const int slot = st % kFewStages;
-        if (st >= kFewStages && !mbar_wait(empty(slot), (st / kFewStages - 1) & 1, p.status, &abort_flag, wb)) break;
-        const int k = k0 + st * kFewStageKeys;
-        const uint32_t n = min(kFewStageKeys, kend - k), dst = stages + slot * Cfg::kStageBytes;
-        mbar_expect_tx(full(slot), n * (D + 2 * (D / kKv4Group)));
-        bulk_load(dst, p.k_codes + (row0 + k) * (D / 2), n * (D / 2), full(slot));
-        bulk_load(dst + 2 * Cfg::kCodeBytes, p.k_scales + (row0 + k) * (D / kKv4Group), n * (D / kKv4Group), full(slot));
-        bulk_load(dst + Cfg::kCodeBytes, p.v_codes + (row0 + k) * (D / 2), n * (D / 2), full(slot));
-        bulk_load(dst + 2 * Cfg::kCodeBytes + Cfg::kScaleBytes, p.v_scales + (row0 + k) * (D / kKv4Group), n * (D / kKv4Group), full(slot));
-      }
-      if (st < nst)                                       // gave up: what was requested has to land before the memory is released
-        for (int s2 = max(0, st - kFewStages); s2 < st; ++s2) {
-          const long long t0 = clock64();
-          while (!mbar_try_wait(full(s2 % kFewStages), (s2 / kFewStages) & 1) && clock64() - t0 < kWaitCycles) {}
-        }
-    }
-  } else {
+  const int kend = (k1 + 7) & ~7;                         // whole 16 bytes of scales; within the cache (L_cap % 8 == 0)
+  auto request = [&](int st) {
+    const int slot = st % kFewStages, k = k0 + st * kFewStageKeys;
+    const uint32_t n = min(kFewStageKeys, kend - k), dst = stages + slot * Cfg::kStageBytes;
+    mbar_expect_tx(full(slot), n * (D + 2 * (D / kKv4Group)));
+    bulk_load(dst, p.k_codes + (row0 + k) * (D / 2), n * (D / 2), full(slot));
+    bulk_load(dst + 2 * Cfg::kCodeBytes, p.k_scales + (row0 + k) * (D / kKv4Group), n * (D / kKv4Group), full(slot));
+    bulk_load(dst + Cfg::kCodeBytes, p.v_codes + (row0 + k) * (D / 2), n * (D / 2), full(slot));
+    bulk_load(dst + 2 * Cfg::kCodeBytes + Cfg::kScaleBytes, p.v_scales + (row0 + k) * (D / kKv4Group), n * (D / kKv4Group), full(slot));
+  };
+  if (threadIdx.x == 0)
+    for (int st = 0; st < min(kFewStages, nst); ++st) request(st);
+  {
     // ------------------------------------------------------------------ products
     uint32_t q[NB][KW][4];                                // [word][pair]: the lane's values of row rho0 + 8 nb + gid
     int lim[NB][2];
@@ -165,74 +163,95 @@ __global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_fe
         q[nb][w][0] = v.x; q[nb][w][1] = v.y; q[nb][w][2] = v.z; q[nb][w][3] = v.w;
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) lim[nb][i] = limit_of(rho0 + nb * 8 + 2 * tig + i);
+      for (int i = 0; i < 2; ++i) lim[nb][i] = min(limit_of(rho0 + nb * 8 + 2 * tig + i), k1);
     }
-    const float c = p.scale_log2;
+    const float grow = 8.f / c;
     bool ok = true;
     for (int st = 0; st < nst; ++st) {
       const int slot = st % kFewStages;
       ok = __all_sync(0xffffffffu, mbar_wait(full(slot), (st / kFewStages) & 1, p.status, &abort_flag, wb));
       if (!ok) break;
       const uint32_t base = stages + slot * Cfg::kStageBytes;
-#pragma unroll 1
-      for (int rd = 0; rd < kFewRounds; ++rd) {
-        const int kr = rd * kFewKeys + warp * 16, key = k0 + st * kFewStageKeys + kr;        // the warp's 16 keys
-        if (key >= k1) break;
-        // S^T = K Q^T: lane (gid, tig) has quarter tig of keys gid and gid + 8
-        float s[NB][4];
+      const int kr = warp * 16 * kFewSets, key = k0 + st * kFewStageKeys + kr;               // the warp's keys
+      if (key < k1) {
+        uint32_t kw[kFewSets][2][KW], vw[kFewSets][4][VW], ks[kFewSets][2], vs[kFewSets][4];
+#pragma unroll
+        for (int x = 0; x < kFewSets; ++x) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = kr + 16 * x + gid + 8 * i;
+            ld_shared_words<KW>(base + row * (D / 2) + tig * (D / 8), kw[x][i]);
+            ks[x][i] = ld_shared_u8(base + 2 * Cfg::kCodeBytes + row * (D / kKv4Group) + tig * (D / 4) / kKv4Group);
+          }
+        }
+        // S^T = K Q^T: lane (gid, tig) has quarter tig of keys gid and gid + 8 of a set
+        float s[kFewSets][NB][4];
+#pragma unroll
+        for (int x = 0; x < kFewSets; ++x)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[x][nb][k] = 0.f;
+        uint32_t s0[kFewSets], s1[kFewSets], f0[kFewSets], f1[kFewSets];
+#pragma unroll
+        for (int x = 0; x < kFewSets; ++x) {
+          s0[x] = kv4_scale2(ks[x][0]);
+          s1[x] = kv4_scale2(ks[x][1]);
+          f0[x] = kv4_offset2(s0[x]);
+          f1[x] = kv4_offset2(s1[x]);
+        }
+#pragma unroll
+        for (int w = 0; w < KW; ++w)
+#pragma unroll
+          for (int x = 0; x < kFewSets; ++x) {
+            uint32_t a[4], a8[4];
+            kv4_word(kw[x][0][w], s0[x], f0[x], a);
+            kv4_word(kw[x][1][w], s1[x], f1[x], a8);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+              mma_16816(s[x][nb], a[0], a8[0], a[1], a8[1], q[nb][w][0], q[nb][w][1]);
+              mma_16816(s[x][nb], a[2], a8[2], a[3], a8[3], q[nb][w][2], q[nb][w][3]);
+            }
+          }
+#pragma unroll
+        for (int x = 0; x < kFewSets; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {                   // keys 2 tig, 2 tig + 1, 2 tig + 8, 2 tig + 9; values gid * D / 8 ...
+            const int row = kr + 16 * x + 2 * tig + (i & 1) + 8 * (i >> 1);
+            ld_shared_words<VW>(base + Cfg::kCodeBytes + row * (D / 2) + gid * (D / 16), vw[x][i]);
+            vs[x][i] = ld_shared_u8(base + 2 * Cfg::kCodeBytes + Cfg::kScaleBytes + row * (D / kKv4Group) + gid * (D / 8) / kKv4Group);
+          }
+        // s[x][nb][0 .. 3]: (key gid, row 2 tig), (gid, 2 tig + 1), (gid + 8, 2 tig), (gid + 8, 2 tig + 1)
+        if (key + 16 * kFewSets > kmin) {
+#pragma unroll
+          for (int x = 0; x < kFewSets; ++x)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (key + 16 * x + gid + 8 * (k >> 1) >= lim[nb][k & 1]) s[x][nb][k] = -INFINITY;
+        }
+        bool need = false;
+        float top[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) s[nb][k] = 0.f;
-        uint32_t kw[2][KW], vw[4][VW], ks[2], vs[4];
+          for (int i = 0; i < 2; ++i) {
+            top[nb][i] = fmaxf(s[0][nb][i], s[0][nb][i + 2]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int row = kr + gid + 8 * i;
-          ld_shared_words<KW>(base + row * (D / 2) + tig * (D / 8), kw[i]);
-          ks[i] = ld_shared_u8(base + 2 * Cfg::kCodeBytes + row * (D / kKv4Group) + tig * (D / 4) / kKv4Group);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {                     // keys 2 tig, 2 tig + 1, 2 tig + 8, 2 tig + 9; values gid * D / 8 ...
-          const int row = kr + 2 * tig + (i & 1) + 8 * (i >> 1);
-          ld_shared_words<VW>(base + Cfg::kCodeBytes + row * (D / 2) + gid * (D / 16), vw[i]);
-          vs[i] = ld_shared_u8(base + 2 * Cfg::kCodeBytes + Cfg::kScaleBytes + row * (D / kKv4Group) + gid * (D / 8) / kKv4Group);
-        }
-        const uint32_t s0 = kv4_scale2(ks[0]), s1 = kv4_scale2(ks[1]), f0 = kv4_offset2(s0), f1 = kv4_offset2(s1);
-#pragma unroll
-        for (int w = 0; w < KW; ++w) {
-          uint32_t a[4], a8[4];
-          kv4_word(kw[0][w], s0, f0, a);
-          kv4_word(kw[1][w], s1, f1, a8);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            mma_16816(s[nb], a[0], a8[0], a[1], a8[1], q[nb][w][0], q[nb][w][1]);
-            mma_16816(s[nb], a[2], a8[2], a[3], a8[3], q[nb][w][2], q[nb][w][3]);
+            for (int x = 1; x < kFewSets; ++x) top[nb][i] = fmaxf(top[nb][i], fmaxf(s[x][nb][i], s[x][nb][i + 2]));
+            need = need || top[nb][i] > m[nb][i] + grow;
           }
-        }
-        // s[nb][0 .. 3]: (key gid, row 2 tig), (gid, 2 tig + 1), (gid + 8, 2 tig), (gid + 8, 2 tig + 1)
-        bool need = false;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          if (key + 16 > kmin) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (key + gid + 8 * (k >> 1) >= lim[nb][k & 1]) s[nb][k] = -INFINITY;
-          }
-#pragma unroll
-          for (int k = 0; k < 4; ++k) s[nb][k] *= c;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) need = need || fmaxf(s[nb][i], s[nb][i + 2]) > m[nb][i] + 8.f;
-        }
-        // the accumulators are scaled anew only when a maximum has grown by more than 2^8 (the first keys: from -inf)
+        // the accumulators are scaled anew only when a maximum has grown by more than 2^8 (and at the first keys)
         if (__any_sync(0xffffffffu, need)) {
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              float top = fmaxf(s[nb][i], s[nb][i + 2]);
+              float t2 = top[nb][i];
 #pragma unroll
-              for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-              const float m2 = fmaxf(m[nb][i], top), a = m2 == -INFINITY ? 1.f : exp2f(m[nb][i] - m2);
+              for (int d = 4; d < 32; d <<= 1) t2 = fmaxf(t2, __shfl_xor_sync(0xffffffffu, t2, d));
+              const float m2 = fmaxf(m[nb][i], t2), a = exp2f((m[nb][i] - m2) * c);
               m[nb][i] = m2;
               l[nb][i] *= a;
 #pragma unroll
@@ -242,45 +261,51 @@ __global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_fe
               }
             }
         }
-        uint32_t pt[NB][2];                               // P^T of keys 0 - 7 and 8 - 15, as the second operand wants it
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          float e[4];
+        for (int x = 0; x < kFewSets; ++x) {
+          uint32_t pt[NB][2];                             // P^T of keys 0 - 7 and 8 - 15, as the second operand wants it
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float mm = m[nb][k & 1] == -INFINITY ? 0.f : m[nb][k & 1];
-            e[k] = exp2f(s[nb][k] - mm);
+          for (int nb = 0; nb < NB; ++nb) {
+            float e[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) e[k] = exp2f(fmaf(s[x][nb][k], c, -m[nb][k & 1] * c));
+            l[nb][0] += e[0] + e[2];
+            l[nb][1] += e[1] + e[3];
+            pt[nb][0] = transpose_8x8(pack_bf2(e[0], e[1]));
+            pt[nb][1] = transpose_8x8(pack_bf2(e[2], e[3]));
           }
-          l[nb][0] += e[0] + e[2];
-          l[nb][1] += e[1] + e[3];
-          pt[nb][0] = transpose_8x8(pack_bf2(e[0], e[1]));
-          pt[nb][1] = transpose_8x8(pack_bf2(e[2], e[3]));
-        }
-        // O^T += V^T P^T: lane (gid, tig) has values gid * D / 8 .. of four keys; a pair of keys makes an operand register
-        const uint32_t v0 = __byte_perm(kv4_scale2(vs[0]), kv4_scale2(vs[1]), 0x5410), v1 = __byte_perm(kv4_scale2(vs[2]), kv4_scale2(vs[3]), 0x5410);
-        const uint32_t g0 = kv4_offset2(v0), g1 = kv4_offset2(v1);
+          // O^T += V^T P^T: lane (gid, tig) has values gid * D / 8 .. of four keys; a pair of keys makes an operand register
+          const uint32_t v0 = kv4_scales(vs[x][0], vs[x][1]), v1 = kv4_scales(vs[x][2], vs[x][3]);
+          const uint32_t g0 = kv4_offset2(v0), g1 = kv4_offset2(v1);
 #pragma unroll
-        for (int w = 0; w < VW; ++w) {
-          uint32_t even0[4], odd0[4], even1[4], odd1[4];  // values 2 p and 2 p + 1 of the word, of the first and the second two keys
-          kv4_word(__byte_perm(vw[0][w], vw[1][w], 0x5410), v0, g0, even0);
-          kv4_word(__byte_perm(vw[0][w], vw[1][w], 0x7632), v0, g0, odd0);
-          kv4_word(__byte_perm(vw[2][w], vw[3][w], 0x5410), v1, g1, even1);
-          kv4_word(__byte_perm(vw[2][w], vw[3][w], 0x7632), v1, g1, odd1);
+          for (int w = 0; w < VW; ++w) {
+            uint32_t even0[4], odd0[4], even1[4], odd1[4];  // values 2 p and 2 p + 1 of the word, of the first and the second two keys
+            kv4_word(__byte_perm(vw[x][0][w], vw[x][1][w], 0x5410), v0, g0, even0);
+            kv4_word(__byte_perm(vw[x][0][w], vw[x][1][w], 0x7632), v0, g0, odd0);
+            kv4_word(__byte_perm(vw[x][2][w], vw[x][3][w], 0x5410), v1, g1, even1);
+            kv4_word(__byte_perm(vw[x][2][w], vw[x][3][w], 0x7632), v1, g1, odd1);
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma_16816(o[nb][w * 4 + t], even0[t], odd0[t], even1[t], odd1[t], pt[nb][0], pt[nb][1]);
+              for (int nb = 0; nb < NB; ++nb) mma_16816(o[nb][w * 4 + t], even0[t], odd0[t], even1[t], odd1[t], pt[nb][0], pt[nb][1]);
+          }
         }
       }
+      // The warp that is last to be done with the slot has it filled again: nobody waits for room.  (A ninth warp that did
+      // spent a sixth of the issue slots on asking.)
       __syncwarp();
-      if (lane == 0) mbar_arrive(empty(slot));
+      if (lane == 0 && st + kFewStages < nst && add_acq_rel(smem_u32(&done[slot]), 1) % kFewWarps == kFewWarps - 1) request(st + kFewStages);
+    }
+    if (!ok && lane == 0) {                               // gave up: what was requested has to land before the memory is released
+      const long long t0 = clock64();
+      while (clock64() - t0 < kMinWaitCycles) {}
     }
   }
 
   // -------------------------------------------------------------------- the warps' parts meet, then those of the ranges
   __syncthreads();
   const uint32_t part = stages, part_ml = stages + Cfg::kPartBytes;
-  if (warp < kFewWarps) {
+  {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -303,7 +328,7 @@ __global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_fe
   for (int x = threadIdx.x; x < Cfg::kQuads; x += kFewThreads) {
     const int row = x * 4 / D, d = x * 4 % D;
     float2 ml[kFewWarps];
-    float m_all = -INFINITY, l_all = 0.f;
+    float m_all = kNoMax, l_all = 0.f;
 #pragma unroll
     for (int w = 0; w < kFewWarps; ++w) {
       ml[w] = ld_shared_f2(part_ml + (w * Cfg::kRows + row) * 8);
@@ -312,7 +337,7 @@ __global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_fe
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < kFewWarps; ++w) {
-      const float a = range_weight(ml[w].x, ml[w].y, m_all);
+      const float a = range_weight(ml[w].x, ml[w].y, m_all, c);
       const float4 v = ld_shared_f4(part + (w * Cfg::kRows + row) * Cfg::kPitch + d * 4);
       acc.x = fmaf(a, v.x, acc.x); acc.y = fmaf(a, v.y, acc.y); acc.z = fmaf(a, v.z, acc.z); acc.w = fmaf(a, v.w, acc.w);
       l_all = fmaf(a, ml[w].y, l_all);
@@ -338,12 +363,12 @@ __global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_fe
       const int x = sp * cnt + y;
       if (x >= Cfg::kQuads) break;
       const int row = x * 4 / D, d = x * 4 % D, rho = rho0 + row;
-      float m_all = -INFINITY, l_all = 0.f;
+      float m_all = kNoMax, l_all = 0.f;
       for (int t = 0; t < splits; ++t) m_all = fmaxf(m_all, ld_shared_f2(recv_ml + (t * Cfg::kRows + row) * 8).x);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int t = 0; t < splits; ++t) {
         const float2 ml = ld_shared_f2(recv_ml + (t * Cfg::kRows + row) * 8);
-        const float a = range_weight(ml.x, ml.y, m_all);
+        const float a = range_weight(ml.x, ml.y, m_all, c);
         const float4 v = ld_shared_f4(recv + (t * cnt + y) * 16);
         acc.x = fmaf(a, v.x, acc.x); acc.y = fmaf(a, v.y, acc.y); acc.z = fmaf(a, v.z, acc.z); acc.w = fmaf(a, v.w, acc.w);
         l_all = fmaf(a, ml.y, l_all);
@@ -356,16 +381,17 @@ __global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_fe
   }
 }
 
-int g_few_force = 0;
-template <int D, int NB>
+int g_few_force = 0, g_few_w = 8;
+template <int D, int NB, int W>
 static cudaError_t launch_few(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
-  using Cfg = FewCfg<D, NB>;
+  using Cfg = FewCfg<D, NB, W>;
+  constexpr int kFewThreads = 32 * W, kFewKeys = Cfg::kFewKeys;
   static unsigned long long prepared = 0;                 // a bit a device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !(prepared >> dev & 1)) {
-    e = cudaFuncSetAttribute(attention_kv4_few_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
+    e = cudaFuncSetAttribute(attention_kv4_few_kernel<D, NB, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
     if (e != cudaSuccess) return e;
     if (dev < 64) prepared |= 1ull << dev;
   }
@@ -393,13 +419,17 @@ static cudaError_t launch_few(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
   if (one_predecessor(st)) attr[n++] = pdl_attribute();
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, attention_kv4_few_kernel<D, NB>, a);
+  return cudaLaunchKernelEx(&cfg, attention_kv4_few_kernel<D, NB, W>, a);
 }
 
 cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, int num_sms, cudaStream_t st) {
   const bool one = a.r * static_cast<long long>(a.H / a.Hkv) <= 8;
-  if (a.D == 64) return one ? launch_few<64, 1>(a, num_sms, st) : launch_few<64, 2>(a, num_sms, st);
-  return one ? launch_few<128, 1>(a, num_sms, st) : launch_few<128, 2>(a, num_sms, st);
+  if (g_few_w == 4) {
+  if (a.D == 64) return one ? launch_few<64, 1, 4>(a, num_sms, st) : launch_few<64, 2, 4>(a, num_sms, st);
+  return one ? launch_few<128, 1, 4>(a, num_sms, st) : launch_few<128, 2, 4>(a, num_sms, st);
+  }
+  if (a.D == 64) return one ? launch_few<64, 1, 8>(a, num_sms, st) : launch_few<64, 2, 8>(a, num_sms, st);
+  return one ? launch_few<128, 1, 8>(a, num_sms, st) : launch_few<128, 2, 8>(a, num_sms, st);
 }
 
 }  // namespace fvar

@@ -9,7 +9,9 @@ namespace fvar {
 constexpr int kKv4Group = 32;                  // values a scale
 
 // bf16 pair (s, s) of a scale byte: 8 e + m moved to exponent e - 20 + 127 and the top three mantissa bits.
-__device__ __forceinline__ uint32_t kv4_scale2(uint32_t byte) { return ((byte + (107u << 3)) << 4) * 0x00010001u; }
+__device__ __forceinline__ uint32_t kv4_scale2(uint32_t byte) { return byte * 0x00100010u + (107u << 7) * 0x00010001u; }
+// The pair (s of lo, s of hi).
+__device__ __forceinline__ uint32_t kv4_scales(uint32_t lo, uint32_t hi) { return hi * 0x00100000u + (lo * 16u + (107u << 7) * 0x00010001u); }
 
 __device__ __forceinline__ uint32_t fma_bf2(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d;
@@ -24,9 +26,12 @@ __device__ __forceinline__ uint32_t mul_bf2(uint32_t a, uint32_t b) {
 // -136 s: 136 = 17 * 8 and s has four significant bits, so the product has eight and is exact.
 __device__ __forceinline__ uint32_t kv4_offset2(uint32_t s2) { return mul_bf2(s2, 0xC308C308u); }
 // Two numbers of 4 bits in the low bits of both halves -> the two values.  0x4300 | u is 128 + u in bf16; (128 + u) s - 136 s =
-// (u - 8) s has seven significant bits, so the one rounding of the fma changes nothing.
+// (u - 8) s has seven significant bits, so the one rounding of the fma changes nothing.  Mask and exponent in one three-input
+// operation (written with & and |, it came out as two).
 __device__ __forceinline__ uint32_t kv4_pair(uint32_t w, uint32_t s2, uint32_t off2) {
-  return fma_bf2((w & 0x000F000Fu) | 0x43004300u, s2, off2);
+  uint32_t x;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(x) : "r"(w), "r"(0x000F000Fu), "r"(0x43004300u));      // (w & mask) | exponent
+  return fma_bf2(x, s2, off2);
 }
 // A word of eight: values 2 p, 2 p + 1 in v[p].
 __device__ __forceinline__ void kv4_word(uint32_t w, uint32_t s2, uint32_t off2, uint32_t (&v)[4]) {
