@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libfvar.so")
 CALLS = os.path.join(HERE, "_calls.so")
 HEADER = os.path.join(HERE, "..", "include", "fvar.h")
 OBJDIR = os.path.join(HERE, "_build")
-SOURCES = ("gemm.cu", "gemm_pair.cu", "gemm_skinny.cu", "gemm_flex.cu", "attention.cu", "attention_kv4.cu", "kv4.cu", "elementwise.cu", "transition.cu", "lls.cu", "fvar_api.cu", "no_alloc.cu", "schedule.cu")
+SOURCES = ("gemm.cu", "gemm_pair.cu", "gemm_skinny.cu", "gemm_flex.cu", "attention.cu", "attention_kv4.cu", "attention_kv4_many.cu", "kv4.cu", "elementwise.cu", "transition.cu", "lls.cu", "fvar_api.cu", "no_alloc.cu", "schedule.cu")
 NVCC_FLAGS = os.environ.get("FVAR_NVCC_EXTRA", "").split() + ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--use_fast_math", "-Xptxas", "-v"]
 

@@ -1,0 +1,644 @@
+// Attention over a cache in 4 bits for many query rows (format and operator: include/fvar.h), on the fifth-generation tensor cores.
+//
+// A unit of work is up to 256 query rows (two tiles of 128) of one cache head of one element; with grouped heads the rows of all
+// heads of the group, rho = row * G + head of the group.  One CTA of 16 warps:
+//   warp 0        issues S_t = Q_t K^T and O_t += P_t V, accumulators in TMEM;
+//   warps 4-7     decode: the codes of 128 keys come from memory into registers two tiles ahead, and leave as the bf16 operand tile,
+//                 swizzled, in a ring of shared-memory slots; they also bring the queries;
+//   warps 8-11, 12-15   softmax of stream 0 and 1, one query row a thread.
+// The two streams are the two query tiles, out of phase, or with a lone tile the even and the odd blocks of keys.  A decoded
+// tile serves both query tiles.  Keys and values have the same layout, rows of D: the keys are a K-major operand, the values an
+// MN-major one, so neither is transposed.  The softmax is that of attention.cu (P in TMEM, two halves, rescaling only when a maximum has
+// grown by 2^8).  Every wait is bounded.
+//
+// Few units over many keys: the key range is split over a cluster of up to 6 CTAs, whose rows are pushed to the CTA that merges them
+// and added up in range order.
+#include <limits.h>
+#include <math.h>
+
+#include "kv4.cuh"
+#include "ptx.cuh"
+#include "softmax.cuh"
+
+namespace fvar {
+
+constexpr int kManyThreads = 512;
+constexpr int kDecodeWarp = 4, kManySoftmaxWarp = 8;
+constexpr int kRegsMma = 40, kRegsDecode = 104, kRegsRows = 184;     // registers a thread after the split: 40 + 104 + 2 * 184 = 4 * 128
+constexpr int kTileRows = 128, kBlockKeys = 128;
+constexpr int kAtom = 128 * 128;              // [128 rows][64 bf16], swizzled
+constexpr float kGrow = 8.0f;                 // log2 units
+constexpr float kNoRowMax = -3.0e38f;         // running maxima start here: finite, so that no difference of two of them is a NaN
+constexpr int kManyMaxRanges = 6;
+
+template <int D>
+struct ManyCfg {
+  static constexpr int kTileBytes = 128 * D * 2;          // a query tile, a tile of 128 keys or of their values
+  static constexpr int kRing = D == 64 ? 10 : 5;
+  static constexpr int kQBytes = 2 * kTileBytes, kSwapBytes = 2 * kTileRows * 8;
+  static constexpr int kBars = 12 + 2 * kRing;
+  static constexpr int kSmemBytes = kQBytes + kRing * kTileBytes + kSwapBytes + 320;
+  static constexpr int kTmemCols = 512;                   // S0, S1, O0, O1
+  static_assert(kBars * 8 + 16 <= 320 && kSmemBytes <= 232448, "shared memory");
+  static_assert(kSmemBytes > 116 * 1024, "one CTA per SM (the CTA allocates all of TMEM)");
+};
+
+template <int D, bool RANGES>
+__global__ void __launch_bounds__(kManyThreads, 1) attention_kv4_many_kernel(const __grid_constant__ Kv4AttnArgs p) {
+  using Cfg = ManyCfg<D>;
+  constexpr int NR = Cfg::kRing;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t q_smem = smem_u32(smem_raw), ring_smem = q_smem + Cfg::kQBytes, swap_smem = ring_smem + NR * Cfg::kTileBytes;
+  const uint32_t bar_base = swap_smem + Cfg::kSwapBytes;
+  uint8_t *tail = smem_raw + Cfg::kQBytes + NR * Cfg::kTileBytes + Cfg::kSwapBytes + 8 * Cfg::kBars;
+  uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(tail);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 4);
+  const uint32_t q_full = bar_base, q_empty = bar_base + 8;
+  auto ring_full = [&](int s) { return bar_base + 8u * (2 + s); };
+  auto ring_empty = [&](int s) { return bar_base + 8u * (2 + NR + s); };
+  auto s_full = [&](int t) { return bar_base + 8u * (2 + 2 * NR + t); };
+  auto p_half = [&](int t) { return bar_base + 8u * (4 + 2 * NR + t); };
+  auto p_full = [&](int t) { return bar_base + 8u * (6 + 2 * NR + t); };
+  auto o_full = [&](int t) { return bar_base + 8u * (8 + 2 * NR + t); };   // P V of a block that is not the stream's last
+  auto o_last = [&](int t) { return bar_base + 8u * (10 + 2 * NR + t); };
+
+  if (q_smem & 1023) {                                    // the swizzle counts from 1024-byte boundaries
+    if (threadIdx.x == 0) atomicOr(p.status, kStatusTimeout);
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long wb = wait_budget(p.wait_cycles);
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    mbar_init(q_full, 128);
+    mbar_init(q_empty, 1);
+    for (int s = 0; s < NR; ++s) {
+      mbar_init(ring_full(s), 128);
+      mbar_init(ring_empty(s), 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(s_full(t), 1);
+      mbar_init(p_half(t), 128);
+      mbar_init(p_full(t), 128);
+      mbar_init(o_full(t), 1);
+      mbar_init(o_last(t), 1);
+    }
+    mbar_fence_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(smem_u32(tmem_holder), Cfg::kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_holder;
+  pdl_launch_dependents();
+  pdl_wait();
+
+  // Units: RANGES: the CTAs of a cluster take the key ranges of one; else a CTA walks the units blockIdx.x, + gridDim.x, ...
+  const int splits = RANGES ? p.kv_splits : 1, sp = RANGES ? static_cast<int>(blockIdx.x) % splits : 0;
+  const int unit0 = RANGES ? static_cast<int>(blockIdx.x) / splits : blockIdx.x, unit_step = RANGES ? p.units : gridDim.x;
+  const int G = p.H / p.Hkv, nrows = p.r * G;
+  struct Unit {
+    int rho0, h, e, ntiles, kb0, nkv, keys;               // keys: those that some row of the unit sees; blocks [kb0, kb0 + nkv) here
+  };
+  auto unit_at = [&](int u) {
+    Unit x;
+    const int g = fast_div(u, p.div_nqt), qt = u - g * static_cast<int>(p.div_nqt.d);       // neighbouring units share keys and values (L2)
+    x.e = fast_div(g, p.div_h);
+    x.h = g - x.e * p.Hkv;
+    x.rho0 = qt * p.tiles_per_cta * kTileRows;
+    x.ntiles = (p.tiles_per_cta == 2 && nrows - x.rho0 > kTileRows) ? 2 : 1;
+    x.keys = p.L;
+    if (p.limits) {
+      const int i0 = x.rho0 / G, i1 = (min(nrows, x.rho0 + x.ntiles * kTileRows) - 1) / G;
+      int top = 0;
+      for (int i = i0 + lane; i <= i1; i += 32) top = max(top, p.limits[static_cast<long long>(x.e) * p.r + i]);
+      x.keys = min(__reduce_max_sync(0xffffffffu, top), p.L);
+    }
+    const int blocks = (x.keys + kBlockKeys - 1) / kBlockKeys, per = (blocks + splits - 1) / splits;
+    x.kb0 = min(sp * per, blocks);
+    x.nkv = min(per, blocks - x.kb0);
+    return x;
+  };
+  // Item i of a unit's stream of operand tiles: keys (v = 0) or values of which block.  A lone tile has two blocks under way.
+  auto item_at = [](int i, int nkv, bool dual, int &j, int &v) {
+    j = i >> 1, v = i & 1;                                // K 0, V 0, K 1, V 1, ...
+    if (dual && nkv > 1) {                                // K 0, K 1, V 0, K 2, V 1, K 3, ... V nkv-2, V nkv-1
+      const int k = i - 2, alt = 2 * (nkv - 2);
+      v = k >= alt || (k >= 0 && (k & 1) == 0);
+      j = k < 0 ? i : k < alt ? (k >> 1) + (v ? 0 : 2) : k - alt + nkv - 2;
+    }
+  };
+  float m_ref = kNoRowMax, l_run = 0.f;       // softmax threads: running maximum and sum of this thread's query row and stream
+  bool final_ok = true, any_block = false;    // softmax threads: the stream's last P V has completed; there was one
+
+  if (warp < kDecodeWarp) {
+    setmaxnreg_dec<kRegsMma>();
+    if (warp == 0) {
+      // ---------------------------------------------------------------- MMA issuer: the whole warp walks, one lane issues
+      constexpr uint32_t idesc_s = umma_idesc_bf16(kTileRows, kBlockKeys);
+      constexpr uint32_t idesc_o = umma_idesc_bf16(kTileRows, D) | (1u << 16);       // bit 16: the values are MN-major
+      const uint32_t leader = elect_one() ? 1u : 0u;
+      auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status, abort_flag, wb)) != 0; };
+      const uint64_t q_desc = smem_desc_sw128(q_smem), k_desc = smem_desc_sw128(ring_smem), v_desc = smem_desc_sw128_mn(ring_smem, kAtom);
+      auto issue_s = [&](int t, int qt, int slot) {       // S buffer t = Q_qt K^T
+        const uint64_t dq = q_desc + static_cast<uint32_t>(qt * (Cfg::kTileBytes >> 4)), dk = k_desc + static_cast<uint32_t>(slot * (Cfg::kTileBytes >> 4));
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          constexpr uint32_t a = kAtom >> 4;
+          umma_bf16_if(leader, tmem_base + t * kBlockKeys, dq + ((k / 4) * a + 2 * (k % 4)), dk + ((k / 4) * a + 2 * (k % 4)), idesc_s, k != 0);
+        }
+        umma_commit_if(leader, s_full(t));
+      };
+      auto issue_pv = [&](int t, int slot, int half, bool accumulate) {     // O_t (+)= P_t V over 64 keys
+        const uint64_t dv = v_desc + static_cast<uint32_t>(slot * (Cfg::kTileBytes >> 4) + half * (64 * 128 >> 4));
+        const uint32_t to = tmem_base + 256 + t * D, tp = tmem_base + t * kBlockKeys + half * 32;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) umma_bf16_tmem_a_if(leader, to, tp + 8 * k, dv + k * (16 * 128 >> 4), idesc_o, (accumulate || k != 0) ? 1u : 0u);
+      };
+      bool ok = true;
+      uint32_t q_par = 0, p_par = 0, phase = 0;           // p_par: a bit a stream
+      int slot = 0;
+      auto take = [&]() {                                 // the next tile of the ring; its slot
+        const int s = slot;
+        ok = ok && wait(ring_full(s), phase);
+        tc_fence_after();
+        if (++slot == NR) { slot = 0; phase ^= 1u; }
+        return s;
+      };
+      // P V of the next block of stream t over the values in slot `vs` (taken when first needed)
+      auto pv = [&](int t, int &vs, bool accumulate, bool last) {
+        ok = ok && wait(p_half(t), p_par >> t & 1u);
+        if (vs < 0) vs = take();
+        if (!ok) return;
+        tc_fence_after();
+        issue_pv(t, vs, 0, accumulate);
+        ok = wait(p_full(t), p_par >> t & 1u);
+        if (!ok) return;
+        p_par ^= 1u << t;
+        tc_fence_after();
+        issue_pv(t, vs, 1, true);
+        umma_commit_if(leader, last ? o_last(t) : o_full(t));
+      };
+      for (int u = unit0; ok && u < p.units; u += unit_step) {
+        const Unit x = unit_at(u);
+        const int nkv = x.nkv;
+        if (nkv == 0) continue;
+        ok = wait(q_full, q_par);
+        q_par ^= 1u;
+        if (!ok) break;
+        int ks = take();
+        if (!ok) break;
+        issue_s(0, 0, ks);
+        if (x.ntiles == 2) issue_s(1, 1, ks);
+        umma_commit_if(leader, ring_empty(ks));
+        if (nkv == 1) umma_commit_if(leader, q_empty);
+        if (x.ntiles == 2) {
+          for (int j = 0; ok && j < nkv; ++j) {
+            int vs = -1;
+            ks = -1;
+            for (int t = 0; ok && t < 2; ++t) {
+              pv(t, vs, j > 0, j + 1 == nkv);
+              if (!ok) break;
+              if (t == 1) umma_commit_if(leader, ring_empty(vs));
+              if (j + 1 < nkv) {
+                if (t == 0) ks = take();
+                if (!ok) break;
+                issue_s(t, t, ks);
+                if (t == 1) {
+                  umma_commit_if(leader, ring_empty(ks));
+                  if (j + 2 == nkv) umma_commit_if(leader, q_empty);
+                }
+              }
+            }
+          }
+        } else {
+          if (nkv > 1) {
+            ks = take();
+            if (!ok) break;
+            issue_s(1, 0, ks);
+            umma_commit_if(leader, ring_empty(ks));
+            if (nkv == 2) umma_commit_if(leader, q_empty);
+          }
+          for (int j = 0; ok && j < nkv; ++j) {
+            const int t = j & 1;
+            int vs = -1;
+            pv(t, vs, j > 1, j + 2 >= nkv);
+            if (!ok) break;
+            umma_commit_if(leader, ring_empty(vs));
+            if (j + 2 < nkv) {
+              ks = take();
+              if (!ok) break;
+              issue_s(t, 0, ks);
+              umma_commit_if(leader, ring_empty(ks));
+              if (j + 3 == nkv) umma_commit_if(leader, q_empty);
+            }
+          }
+        }
+      }
+    }
+  } else if (warp < kManySoftmaxWarp) {
+    // ------------------------------------------------------------------ decode
+    setmaxnreg_dec<kRegsDecode>();
+    const int dt = static_cast<int>(threadIdx.x) - 32 * kDecodeWarp, dw = dt >> 5;
+    // A lane decodes 32 values (one group) of a row at a time, eight neighbouring lanes eight neighbouring rows: the stores of a
+    // quarter of a warp then fall into eight different 16-byte columns of the swizzled tile.
+    constexpr int kPieces = D / 32, kStep = 32 / kPieces, kReps = 32 / kStep;       // rows at a time, times for a warp's 32 rows
+    const int piece = (lane >> 3) % kPieces, lrow = dw * 32 + (lane & 7) + 8 * ((lane >> 3) / kPieces);
+    struct Codes {
+      uint4 w[kReps];
+      uint32_t s[kReps];
+    };
+    bool ok = true;
+    int slot = 0;
+    uint32_t phase = 0, q_units = 0;
+    for (int u = unit0; ok && u < p.units; u += unit_step) {
+      const Unit x = unit_at(u);
+      if (x.nkv == 0) continue;
+      const bool dual = x.ntiles == 1;
+      const long long row0 = x.e * p.elem_stride + static_cast<long long>(x.h) * p.L_cap;
+      auto load = [&](int i, Codes &c) {
+        int j, v;
+        item_at(i, x.nkv, dual, j, v);
+        const int key0 = (x.kb0 + j) * kBlockKeys + lrow;
+        const uint8_t *codes = v ? p.v_codes : p.k_codes, *scales = v ? p.v_scales : p.k_scales;
+#pragma unroll
+        for (int k = 0; k < kReps; ++k) {
+          const int key = key0 + k * kStep;
+          const bool there = i < 2 * x.nkv && key < x.keys;
+          c.w[k] = there ? __ldg(reinterpret_cast<const uint4 *>(codes + (row0 + key) * (D / 2)) + piece) : make_uint4(0, 0, 0, 0);
+          c.s[k] = there ? __ldg(scales + (row0 + key) * (D / kKv4Group) + piece) : 0u;
+        }
+      };
+      auto put = [&](const Codes &c) {
+        if (!ok) return;
+        ok = __all_sync(0xffffffffu, mbar_wait(ring_empty(slot), phase ^ 1u, p.status, abort_flag, wb));
+        if (!ok) return;
+        const uint32_t tile = ring_smem + slot * Cfg::kTileBytes + (piece >> 1) * kAtom;
+#pragma unroll
+        for (int k = 0; k < kReps; ++k) {
+          const int row = lrow + k * kStep;
+          const uint32_t s2 = kv4_scale2(c.s[k]), f2 = kv4_offset2(s2), w[4] = {c.w[k].x, c.w[k].y, c.w[k].z, c.w[k].w};
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            uint32_t o[4];
+            kv4_word(w[n], s2, f2, o);
+            const uint32_t chunk = ((piece & 1) * 4 + n) ^ (row & 7);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile + row * 128 + chunk * 16), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+          }
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(ring_full(slot));
+        if (++slot == NR) { slot = 0; phase ^= 1u; }
+      };
+      Codes a, b;
+      load(0, a);
+      load(1, b);
+      if (q_units > 0) ok = __all_sync(0xffffffffu, mbar_wait(q_empty, (q_units - 1) & 1u, p.status, abort_flag, wb));
+      if (!ok) break;
+      ++q_units;
+      constexpr int kLanes = D / 8;                       // lanes of a query row
+      for (int k = dt; k < x.ntiles * kTileRows * kLanes; k += 128) {
+        const int row = k / kLanes, ch = k % kLanes, rho = x.rho0 + row;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (rho < nrows) v = __ldg(reinterpret_cast<const uint4 *>(p.q + (static_cast<long long>(x.e) * p.r + rho / G) * p.ldq + (x.h * G + rho % G) * D) + ch);
+        const uint32_t dst = q_smem + (row >> 7) * Cfg::kTileBytes + (ch >> 3) * kAtom + (row & 127) * 128 + ((ch ^ row) & 7) * 16;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(q_full);
+      for (int i = 0; ok && i < 2 * x.nkv; i += 2) {
+        put(a);
+        load(i + 2, a);
+        put(b);
+        load(i + 3, b);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax
+    setmaxnreg_inc<kRegsRows>();
+    const int t = (warp - kManySoftmaxWarp) >> 2, quad = warp & 3, row_local = quad * 32 + lane;
+    const uint32_t lane_addr = static_cast<uint32_t>(quad * 32) << 16;
+    const uint32_t s_addr = tmem_base + lane_addr + t * kBlockKeys, o_addr = tmem_base + lane_addr + 256 + t * D;
+    const float c = p.scale_log2;
+    uint32_t s_par = 0, o_base = 0, last_par = 0;         // o_base: commits to o_full(t) so far; last_par: a bit a stream
+    bool ok = true;
+    for (int u = unit0; ok && u < p.units; u += unit_step) {
+      const Unit x = unit_at(u);
+      const bool dual = x.ntiles == 1;
+      const int nblk = dual ? (x.nkv + 1 - t) >> 1 : x.nkv;
+      const int rho = x.rho0 + (dual ? 0 : t * kTileRows) + row_local;
+      m_ref = kNoRowMax;
+      l_run = 0.f;
+      any_block = nblk > 0;
+      int limit = 0;
+      if (rho < nrows) limit = p.limits ? min(p.limits[static_cast<long long>(x.e) * p.r + rho / G], x.keys) : x.keys;
+      for (int j = 0; j < nblk; ++j) {
+        ok = __all_sync(0xffffffffu, mbar_wait(s_full(t), s_par, p.status, abort_flag, wb));
+        if (!ok) break;
+        s_par ^= 1u;
+        tc_fence_after();
+        const int valid = limit - (x.kb0 + (dual ? 2 * j + t : j)) * kBlockKeys;       // keys of this block that the row sees (>= 128: all)
+        uint32_t v[4][32];
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc) tmem_ld32(s_addr + cc * 32, v[cc]);
+        tmem_ld_wait();
+        if (__any_sync(0xffffffffu, valid < kBlockKeys)) {
+#pragma unroll
+          for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (cc * 32 + i >= valid) v[cc][i] = 0xff800000u;   // -inf
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) mx[(i >> 1) & 3] = max3(mx[(i >> 1) & 3], __uint_as_float(v[cc][i]), __uint_as_float(v[cc][i + 1]));
+        const float m_cand = fmaxf(m_ref, fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]));
+        const bool need = (m_cand - m_ref) * c > kGrow;
+        if (__any_sync(0xffffffffu, need)) {
+          if (j > 0) {                                    // O is about to be touched: P V of block j - 1 must be complete
+            ok = __all_sync(0xffffffffu, mbar_wait(o_full(t), (o_base + j - 1) & 1u, p.status, abort_flag, wb));
+            if (!ok) break;
+            tc_fence_after();
+          }
+          const float alpha = need ? exp2f((m_ref - m_cand) * c) : 1.0f;
+          if (need) m_ref = m_cand;
+          l_run *= alpha;
+          if (j > 0) {
+#pragma unroll 1
+            for (int cc = 0; cc < D / 32; ++cc) {
+              uint32_t o[32];
+              tmem_ld32(o_addr + cc * 32, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+              tmem_st32(o_addr + cc * 32, o);
+            }
+            tmem_st_wait();
+          }
+        }
+        const float neg_mc = -m_ref * c;
+        const uint64_t c2 = pack_f2(c, c), neg_mc2 = pack_f2(neg_mc, neg_mc);
+        uint64_t ls[2] = {0ull, 0ull};
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc) {                  // keys 32 cc .. of this row, two a word, over the first columns of S
+          uint32_t pk[16];
+#pragma unroll
+          for (int pr = 0; pr < 16; ++pr) {
+            float p0, p1;
+            unpack_f2(fma_f2(pack_f2(__uint_as_float(v[cc][2 * pr]), __uint_as_float(v[cc][2 * pr + 1])), c2, neg_mc2), p0, p1);
+            p0 = exp2f(p0);
+            p1 = exp2f(p1);
+            ls[pr & 1] = add_f2(ls[pr & 1], pack_f2(p0, p1));
+            const __nv_bfloat162 v2 = __floats2bfloat162_rn(p0, p1);
+            pk[pr] = *reinterpret_cast<const uint32_t *>(&v2);
+          }
+          tmem_st16(s_addr + cc * 16, pk);
+          if (cc & 1) {
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(cc == 1 ? p_half(t) : p_full(t));
+          }
+        }
+        float l0, l1;
+        unpack_f2(add_f2(ls[0], ls[1]), l0, l1);
+        l_run += l0 + l1;
+      }
+      if (!ok) { final_ok = false; break; }
+      if (x.nkv == 0) {                                   // nobody of the unit sees a key (or no key of this range): no product has run
+        if constexpr (!RANGES) {
+          if (t < x.ntiles && rho < nrows) {
+            uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((static_cast<long long>(x.e) * p.r + rho / G) * p.H + x.h * G + rho % G) * D);
+            for (int k = 0; k < D / 8; ++k) dst[k] = make_uint4(0, 0, 0, 0);
+          }
+        }
+        continue;
+      }
+      if (nblk > 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait(o_last(t), last_par >> t & 1u, p.status, abort_flag, wb));
+        final_ok = ok;
+        o_base += nblk - 1;
+      }
+      const bool both = dual && x.nkv > 1;                // the other stream has an accumulator too
+      if constexpr (!RANGES) {
+        // With a lone tile the two streams meet: maxima and sums change sides, and each warp-group finishes half of the columns.
+        float norm = 0.f, other = 0.f;
+        if (dual) {
+          asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(swap_smem + (t * kTileRows + row_local) * 8), "f"(m_ref), "f"(l_run) : "memory");
+          if (t == 1 || both) ok = ok && __all_sync(0xffffffffu, mbar_wait(o_last(t ^ 1), last_par >> (t ^ 1) & 1u, p.status, abort_flag, wb));
+          ok = bar_and(1, 256, ok);
+        }
+        if (ok) {
+          tc_fence_after();
+          if (dual) {
+            const float2 ml = ld_shared_f2(swap_smem + ((t ^ 1) * kTileRows + row_local) * 8);
+            const float m_all = fmaxf(m_ref, ml.x), w0 = exp2f((m_ref - m_all) * c), w1 = exp2f((ml.x - m_all) * c);
+            const float l_all = t == 0 ? fmaf(l_run, w0, ml.y * w1) : fmaf(ml.y, w1, l_run * w0);   // the same sum on both sides
+            const float inv = l_all == 0.f ? 0.f : 1.0f / l_all;
+            norm = w0 * inv;
+            other = w1 * inv;
+          } else {
+            norm = l_run == 0.f ? 0.f : 1.0f / l_run;
+          }
+          int u2 = u;                                     // decoded again: kept in registers through the loop, the unit spills
+          asm volatile("" : "+r"(u2));
+          const int g2 = fast_div(u2, p.div_nqt), e2 = fast_div(g2, p.div_h), h2 = g2 - e2 * p.Hkv;
+          bf16 *dst = p.out + ((static_cast<long long>(e2) * p.r + rho / G) * p.H + h2 * G + rho % G) * D;
+          const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0, there = rho < nrows;
+          const int cc0 = dual ? t * (D / 64) : 0, cc1 = dual ? cc0 + D / 64 : D / 32;
+#pragma unroll 1
+          for (int cc = cc0; cc < cc1; ++cc) {
+            uint32_t v[32];
+            if (nblk > 0) {
+              tmem_ld32(o_addr + cc * 32, v);
+              tmem_ld_wait();
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = 0u;
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * norm);
+            if (dual && (t == 1 || both)) {
+              uint32_t v1[32];
+              tmem_ld32(tmem_base + lane_addr + 256 + (t ^ 1) * D + cc * 32, v1);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(fmaf(__uint_as_float(v1[i]), other, __uint_as_float(v[i])));
+            }
+            if (there) {
+              uint32_t w[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const __nv_bfloat162 v2 = __floats2bfloat162_rn(__uint_as_float(v[i * 2]), __uint_as_float(v[i * 2 + 1]));
+                w[i] = *reinterpret_cast<const uint32_t *>(&v2);
+              }
+              if (wide) {
+                st_global_32(dst + cc * 32, w);
+                st_global_32(dst + cc * 32 + 16, w + 8);
+              } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) reinterpret_cast<uint4 *>(dst + cc * 32)[k] = make_uint4(w[k * 4], w[k * 4 + 1], w[k * 4 + 2], w[k * 4 + 3]);
+              }
+            }
+          }
+          tc_fence_before();
+        }
+        // both halves are out before either warp-group hands over a P of the next unit and so lets an accumulator be overwritten
+        if (dual) asm volatile("bar.sync 1, 256;" ::: "memory");
+      }
+      last_par ^= dual ? (both ? 3u : 1u) : 3u;
+    }
+  }
+
+  if constexpr (RANGES) {
+    // ---------------------------------------------------------------- merge of the key ranges over the cluster
+    // Row slice c of a tile is merged by CTA c.  Every CTA pushes its unnormalised rows (O, m, l) into the shared memory of the slices'
+    // owners, over their rings.  A lone tile has two parts a CTA, one a stream.  All threads pass the same barriers.
+    const Unit x = unit_at(unit0);
+    const bool dual = x.ntiles == 1;
+    const int parts = dual ? 2 * splits : splits;
+    constexpr uint32_t kPitch = (D + 4) * 4;
+    const int rpr0 = (min(kTileRows, nrows - x.rho0) + splits - 1) / splits;
+    const int rpr1 = dual ? 0 : (min(kTileRows, nrows - x.rho0 - kTileRows) + splits - 1) / splits;
+    const int total = parts * (rpr0 + rpr1);              // rows that arrive here, [tile][part][slice row]
+    const uint32_t part_o = ring_smem, part_m = part_o + static_cast<uint32_t>(total) * kPitch;
+    tc_fence_before();
+    __syncwarp();
+    cluster_sync_all();                                   // nobody's ring is in use any more
+    if (warp >= kManySoftmaxWarp && final_ok) {
+      tc_fence_after();
+      const int wg = (warp - kManySoftmaxWarp) >> 2, tile = dual ? 0 : wg, part = dual ? 2 * sp + wg : sp, row = (warp & 3) * 32 + lane;
+      const int rpr = tile == 0 ? rpr0 : rpr1;
+      const uint32_t o_addr = tmem_base + 256 + wg * D + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+      const bool mine = x.rho0 + tile * kTileRows + row < nrows;
+      const int owner = mine ? row / rpr : 0, at = (tile == 0 ? 0 : parts * rpr0) + part * rpr + row - owner * rpr;
+      const uint32_t dst = mapa_shared(part_o + static_cast<uint32_t>(at) * kPitch, static_cast<uint32_t>(owner));
+      const uint32_t dst_m = mapa_shared(part_m + static_cast<uint32_t>(at) * 8u, static_cast<uint32_t>(owner));
+#pragma unroll 1
+      for (int cc = 0; cc < D / 32; ++cc) {
+        uint32_t v[32];
+        if (any_block) {
+          tmem_ld32(o_addr + cc * 32, v);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = 0u;
+        }
+        if (mine) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (cc * 32 + k * 4) * 4), "r"(v[k * 4]), "r"(v[k * 4 + 1]),
+                         "r"(v[k * 4 + 2]), "r"(v[k * 4 + 3]) : "memory");
+        }
+      }
+      if (mine) asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst_m), "f"(m_ref), "f"(l_run) : "memory");
+    }
+    tc_fence_before();
+    __syncwarp();
+    cluster_sync_all();                                   // all rows have arrived; nobody touches a peer after this
+    if (warp >= kManySoftmaxWarp && *abort_flag == 0) {
+      constexpr int kLanes = D / 4;                       // threads a row, one float4 each
+      const int st = static_cast<int>(threadIdx.x) - 32 * kManySoftmaxWarp, d4 = (st % kLanes) * 4;
+      const float c = p.scale_log2;
+#pragma unroll 1
+      for (int k0 = 0; k0 < rpr0 + rpr1; k0 += 256 / kLanes) {       // every lane of a warp goes round as often
+        const bool there = k0 + st / kLanes < rpr0 + rpr1;
+        const int k = there ? k0 + st / kLanes : 0;
+        const int tile = k < rpr0 ? 0 : 1, lrow = tile == 0 ? k : k - rpr0, rpr = tile == 0 ? rpr0 : rpr1;
+        const int rho = x.rho0 + tile * kTileRows + sp * rpr + lrow;
+        const bool live = there && rho < nrows && sp * rpr + lrow < kTileRows;
+        const uint32_t at0 = static_cast<uint32_t>((tile == 0 ? 0 : parts * rpr0) + lrow);
+        // a lane takes one part's maximum and sum; the weights are formed side by side and handed round (12 parts at most)
+        const int l16 = st & 15;
+        const float2 ml = l16 < parts ? ld_shared_f2(part_m + (at0 + l16 * rpr) * 8u) : make_float2(kNoRowMax, 0.f);
+        float m_all = ml.x;
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, d));
+        float w16 = ml.y == 0.f ? 0.f : exp2f((ml.x - m_all) * c), l_all = ml.y * w16;
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) l_all += __shfl_xor_sync(0xffffffffu, l_all, d);
+        w16 *= l_all == 0.f ? 0.f : 1.0f / l_all;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int t2 = 0; t2 < parts; ++t2) {
+          const float w = __shfl_sync(0xffffffffu, w16, t2, 16);
+          const float4 v = ld_shared_f4(part_o + (at0 + t2 * rpr) * kPitch + d4 * 4);
+          o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y); o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w);
+        }
+        if (!live) continue;
+        const __nv_bfloat162 h0 = __floats2bfloat162_rn(o.x, o.y), h1 = __floats2bfloat162_rn(o.z, o.w);
+        *reinterpret_cast<uint2 *>(p.out + ((static_cast<long long>(x.e) * p.r + rho / G) * p.H + x.h * G + rho % G) * D + d4) =
+            make_uint2(*reinterpret_cast<const uint32_t *>(&h0), *reinterpret_cast<const uint32_t *>(&h1));
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, Cfg::kTmemCols);
+  }
+}
+
+template <int D, bool RANGES>
+static cudaError_t many_prepare(int dev) {
+  static unsigned long long prepared = 0;                 // a bit a device
+  if (dev < 64 && (prepared >> dev & 1)) return cudaSuccess;
+  // The register split draws on what the block was launched with: refuse a build whose kernel got fewer.
+  cudaFuncAttributes fa;
+  cudaError_t e = cudaFuncGetAttributes(&fa, attention_kv4_many_kernel<D, RANGES>);
+  if (e != cudaSuccess) return e;
+  if (kManyThreads * fa.numRegs < 128 * (kRegsMma + kRegsDecode + 2 * kRegsRows)) return cudaErrorInvalidConfiguration;
+  e = cudaFuncSetAttribute(attention_kv4_many_kernel<D, RANGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<D>::kSmemBytes);
+  if (e == cudaSuccess && dev < 64) prepared |= 1ull << dev;
+  return e;
+}
+
+int g_many_tiles = 0, g_many_splits = 0;
+
+template <int D>
+static cudaError_t launch_many_d(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const long long rows = static_cast<long long>(a.r) * (a.H / a.Hkv);
+  if (rows > INT_MAX - 256) return cudaErrorInvalidValue;
+  a.tiles_per_cta = g_many_tiles ? g_many_tiles : rows > kTileRows ? 2 : 1;
+  a.kv_splits = g_many_splits ? g_many_splits : 1;
+  const long long nqt = (rows + a.tiles_per_cta * kTileRows - 1) / (a.tiles_per_cta * kTileRows), units = nqt * a.Hkv * a.B;
+  if (units * kManyMaxRanges > INT_MAX) return cudaErrorInvalidValue;
+  a.units = static_cast<int>(units);
+  a.div_nqt = make_fast_div(static_cast<unsigned>(nqt), units);
+  a.div_h = make_fast_div(a.Hkv, units);
+  if (a.kv_splits <= 1) {
+    e = many_prepare<D, false>(dev);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(attention_kv4_many_kernel<D, false>, dim3(a.units < num_sms ? a.units : num_sms), dim3(kManyThreads), ManyCfg<D>::kSmemBytes, st, a);
+  }
+  e = many_prepare<D, true>(dev);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.units * a.kv_splits);
+  cfg.blockDim = dim3(kManyThreads);
+  cfg.dynamicSmemBytes = ManyCfg<D>::kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = a.kv_splits;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1] = pdl_attribute();
+  cfg.attrs = attr;
+  cfg.numAttrs = one_predecessor(st) ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, attention_kv4_many_kernel<D, true>, a);
+}
+
+cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, int num_sms, cudaStream_t st) {
+  return a.D == 64 ? launch_many_d<64>(a, num_sms, st) : launch_many_d<128>(a, num_sms, st);
+}
+
+}  // namespace fvar

@@ -316,8 +316,12 @@ struct Kv4AttnArgs {
   float scale_log2;                       // log2(e) / sqrt(D)
   unsigned *status;
   long long wait_cycles;                  // budget of every bounded wait (0: the default)
-  int kv_splits;                          // ranges of keys, a cluster's CTAs; filled by launch_attention_kv4
+  // Filled by the launch functions: ranges of keys (a cluster's CTAs); query tiles a CTA, units and how they are numbered
+  int kv_splits, tiles_per_cta, units;
+  FastDiv div_nqt, div_h;
 };
+// More than 16 query rows a cache head: tcgen05 (attention_kv4_many.cu).
+cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, int num_sms, cudaStream_t st);
 
 // Self-test of the bounded wait: one CTA waits on an mbarrier nobody signals with a budget of `cycles`, flags the
