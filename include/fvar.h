@@ -419,9 +419,13 @@ fvar_status fvar_kv4_read(const fvar_kv4 *cache, int n, int L0, const int *start
  * cache head h / (H / n_heads).  Row i of element b sees the first min(L, limits[b][i]) rows of its element (limits dev int32
  * [B][r], negative ones count as 0; NULL: the first L rows for every query row).  limits express padded batches, causal rows
  * and the rows of several scales at once, each up to the end of its own scale.  A row that sees nothing becomes 0.
- * 0 <= L <= L_cap; r >= 1. */
+ * 0 <= L <= L_cap; r >= 1.
+ * workspace (dev, 16-byte aligned, workspace_bytes long, used until the call's kernels have run; may be NULL): many query rows are faster when the
+ * keys and values are decoded once into it, which needs fvar_attention_kv4_workspace bytes; with less nothing is written there. */
 fvar_status fvar_attention_kv4(const void *q, long long ldq, const fvar_kv4 *cache, int H, int r, int L, const int *limits, void *out,
-                               void *stream);
+                               void *workspace, size_t workspace_bytes, void *stream);
+/* Bytes of workspace that the call above can use (0: none, or arguments that it refuses).  Host only. */
+size_t fvar_attention_kv4_workspace(const fvar_kv4 *cache, int H, int r, int L);
 
 /* Failure-detection self-test: launches one CTA that waits, with a budget of `cycles` clock cycles, on a
  * barrier nothing ever signals.  The wait gives up, the kernel records FVAR_ETIMEOUT in the status word and

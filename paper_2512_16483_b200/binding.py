@@ -117,7 +117,8 @@ def load_library() -> ct.CDLL:
         "fvar_attention": (i, [vp, vp, vp, i, i, i, i, i, i, vp, vp]),
         "fvar_kv4_write": (i, [P(_Kv4), vp, vp, ll, i, i, vp, vp, vp]),
         "fvar_kv4_read": (i, [P(_Kv4), i, i, vp, vp, vp, vp, vp]),
-        "fvar_attention_kv4": (i, [vp, ll, P(_Kv4), i, i, i, vp, vp, vp]),
+        "fvar_attention_kv4": (i, [vp, ll, P(_Kv4), i, i, i, vp, vp, vp, ct.c_size_t, vp]),
+        "fvar_attention_kv4_workspace": (ct.c_size_t, [P(_Kv4), i, i, i]),
         "fvar_rtr_fill": (i, [vp, i, i, i, i, i, i, vp, vp, vp]),
         "fvar_select_rows_static": (i, [vp, i, i, i, i, vp, vp, vp]),
         "fvar_l2_prefetch": (i, [vp, ct.c_size_t, vp]),
@@ -158,7 +159,7 @@ EXPORTED = ("fvar_workspace_bytes", "fvar_init", "fvar_set_cond", "fvar_set_proj
             "fvar_load_group_cache", "fvar_cache_len", "fvar_launch_count", "fvar_poll_status", "fvar_reset",
             "fvar_destroy", "fvar_last_error", "fvar_restore_loaded", "fvar_set_option", "fvar_profile_enable", "fvar_profile_read", "fvar_profile_dump",
             "fvar_row_scores", "fvar_row_keys", "fvar_select_topr", "fvar_ln_modulate",
-            "fvar_gemm_bf16", "fvar_gemm_bf16_form", "fvar_gemm_bf16_wt", "fvar_cfg_combine", "fvar_attention", "fvar_kv4_write", "fvar_kv4_read", "fvar_attention_kv4", "fvar_rtr_fill", "fvar_select_rows_static", "fvar_l2_prefetch", "fvar_selftest_wait_timeout",
+            "fvar_gemm_bf16", "fvar_gemm_bf16_form", "fvar_gemm_bf16_wt", "fvar_cfg_combine", "fvar_attention", "fvar_kv4_write", "fvar_kv4_read", "fvar_attention_kv4", "fvar_attention_kv4_workspace", "fvar_rtr_fill", "fvar_select_rows_static", "fvar_l2_prefetch", "fvar_selftest_wait_timeout",
             "fvar_rank_from_keep_ratio", "fvar_rank_from_table_ratio", "fvar_infinity_rank_ratio", "fvar_infinity_group_ranks",
             "fvar_infinity_schedule")
 
@@ -314,7 +315,7 @@ class Kv4:
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales    # kept alive
         self.B, self.n_heads, self.L_cap, self.head_dim, self.device = B, H, L_cap, D, k_codes.device
         self._c = _Kv4(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), B, H, D, L_cap, stride)
-        self._ref = ct.byref(self._c)
+        self._ref, self._at, self._dev = ct.byref(self._c), ct.addressof(self._c), self.device.index
 
     @classmethod
     def empty(cls, B: int, n_heads: int, L_cap: int, head_dim: int) -> "Kv4":
@@ -352,6 +353,10 @@ def _current(device):
 def fvar_kv4_write(cache: Kv4, K: torch.Tensor, V: torch.Tensor, start, count: Optional[torch.Tensor] = None):
     """Quantises rows of K, V bf16 [B][n][n_heads * D] into the cache: row i < count[b] to cache row start + i (start an int,
     or int32 [B]).  K and V may be columns of a wider matrix."""
+    res = _native().kv4_write(cache._at, cache._dev, K, V, start, count)
+    if res is not None:
+        _result(res)
+        return
     _current(cache.device)
     ld = _rows_of(K, cache.device)
     assert K.shape == V.shape and K.shape[0] == cache.B and K.shape[2] == cache.n_heads * cache.head_dim, (tuple(K.shape), tuple(V.shape))
@@ -363,6 +368,11 @@ def fvar_kv4_write(cache: Kv4, K: torch.Tensor, V: torch.Tensor, start, count: O
 def fvar_kv4_read(cache: Kv4, n: int, start, count: Optional[torch.Tensor] = None, out=None):
     """Cache rows start .. start + n - 1 as bf16 (K, V), each [B][n][n_heads * D], or into out = (K, V).  Rows at or beyond
     count[b] are left as they were (zero without out)."""
+    if out is not None:
+        res = _native().kv4_read(cache._at, cache._dev, n, start, count, out)
+        if res is not None:
+            _result(res)
+            return out
     _current(cache.device)
     L0, st, cn = _kv4_place(cache, start, count)
     shape = (cache.B, n, cache.n_heads * cache.head_dim)
@@ -379,6 +389,9 @@ def fvar_attention_kv4(q: torch.Tensor, cache: Kv4, L: int, limits: Optional[tor
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """q bf16 [B][r][H * D] over the first L rows of a cache in 4 bits (row i of element b over the first limits[b][i], int32
     [B][r]) -> bf16 [B][r][H * D].  H may be a multiple of the cache's heads; q may be columns of a wider matrix."""
+    res = _native().attention_kv4(cache._at, cache._dev, q, L, limits, out)
+    if res is not None:
+        return _result(res)
     _current(cache.device)
     ld = _rows_of(q, cache.device)
     B, r, C = q.shape
@@ -388,7 +401,10 @@ def fvar_attention_kv4(q: torch.Tensor, cache: Kv4, L: int, limits: Optional[tor
     if out is None:
         out = torch.empty((B, r, C), dtype=torch.bfloat16, device=q.device)
     assert tuple(_dev(out, torch.bfloat16).shape) == (B, r, C) and out.device == cache.device, tuple(out.shape)
-    _check_kernel(load_library().fvar_attention_kv4(q.data_ptr(), ld, cache._ref, C // cache.head_dim, r, L, _ptr(limits), out.data_ptr(), _stream()))
+    lib, H = load_library(), C // cache.head_dim
+    n = lib.fvar_attention_kv4_workspace(cache._ref, H, r, L)
+    work = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    _check_kernel(lib.fvar_attention_kv4(q.data_ptr(), ld, cache._ref, H, r, L, _ptr(limits), out.data_ptr(), _ptr(work), n, _stream()))
     return out
 
 

@@ -423,8 +423,8 @@ static cudaError_t launch_few(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
 }
 
 int g_few_rows = 16;
-cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, int num_sms, cudaStream_t st) {
-  if (a.r * static_cast<long long>(a.H / a.Hkv) > g_few_rows) return launch_attention_kv4_many(a, num_sms, st);
+cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {
+  if (a.r * static_cast<long long>(a.H / a.Hkv) > g_few_rows) return launch_attention_kv4_many(a, workspace, bytes, num_sms, st);
   const bool one = a.r * static_cast<long long>(a.H / a.Hkv) <= 8;
   if (g_few_w == 4) {
   if (a.D == 64) return one ? launch_few<64, 1, 4>(a, num_sms, st) : launch_few<64, 2, 4>(a, num_sms, st);

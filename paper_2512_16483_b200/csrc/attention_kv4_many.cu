@@ -2,10 +2,10 @@
 //
 // A unit of work is up to 256 query rows (two tiles of 128) of one cache head of one element; with grouped heads the rows of all
 // heads of the group, rho = row * G + head of the group.  One CTA of 16 warps:
-//   warp 0        issues S_t = Q_t K^T and O_t += P_t V, accumulators in TMEM;
-//   warps 4-7     decode: the codes of 128 keys come from memory into registers two tiles ahead, and leave as the bf16 operand tile,
-//                 swizzled, in a ring of shared-memory slots; they also bring the queries;
-//   warps 8-11, 12-15   softmax of stream 0 and 1, one query row a thread.
+//   warp 0             issues S_t = Q_t K^T and O_t += P_t V, accumulators in TMEM;
+//   warps 1-7          decode: the codes of 128 keys or their values come from memory into registers a block ahead, and leave as the
+//                      bf16 operand tile, swizzled, in a ring of shared-memory slots; they bring the queries too;
+//   warps 8-11, 12-15  softmax of stream 0 and 1, one query row a thread.
 // The two streams are the two query tiles, out of phase, or with a lone tile the even and the odd blocks of keys.  A decoded
 // tile serves both query tiles.  Keys and values have the same layout, rows of D: the keys are a K-major operand, the values an
 // MN-major one, so neither is transposed.  The softmax is that of attention.cu (P in TMEM, two halves, rescaling only when a maximum has
@@ -13,6 +13,9 @@
 //
 // Few units over many keys: the key range is split over a cluster of up to 6 CTAs, whose rows are pushed to the CTA that merges them
 // and added up in range order.
+//
+// Many query tiles a head: every unit would decode the same keys again, in issue slots that the softmax needs.  Then a pass of its
+// own decodes the cache once into the caller's workspace, and the units (CODES false) request bf16 tiles by TMA.
 #include <limits.h>
 #include <math.h>
 
@@ -22,9 +25,17 @@
 
 namespace fvar {
 
+// bytes a multiple of 16, src 16-byte aligned.
+__device__ __forceinline__ void l2_fetch(const void *src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
+}
+
 constexpr int kManyThreads = 512;
-constexpr int kDecodeWarp = 4, kManySoftmaxWarp = 8;
-constexpr int kRegsMma = 40, kRegsDecode = 104, kRegsRows = 184;     // registers a thread after the split: 40 + 104 + 2 * 184 = 4 * 128
+constexpr int kDecodeWarps = 7, kManySoftmaxWarp = 8;
+// Registers a thread after the split: 2 * 72 + 2 * 184 = 4 * 128.
+constexpr int kRegsLaunch = 128, kRegsDecode = 72, kRegsRows = 184;
+static_assert(2 * kRegsDecode + 2 * kRegsRows == 4 * kRegsLaunch, "what is given back is what is taken");
+constexpr int kFetchAhead = 4;                // blocks
 constexpr int kTileRows = 128, kBlockKeys = 128;
 constexpr int kAtom = 128 * 128;              // [128 rows][64 bf16], swizzled
 constexpr float kGrow = 8.0f;                 // log2 units
@@ -43,8 +54,9 @@ struct ManyCfg {
   static_assert(kSmemBytes > 116 * 1024, "one CTA per SM (the CTA allocates all of TMEM)");
 };
 
-template <int D, bool RANGES>
-__global__ void __launch_bounds__(kManyThreads, 1) attention_kv4_many_kernel(const __grid_constant__ Kv4AttnArgs p) {
+template <int D, bool RANGES, bool CODES>
+__global__ void __launch_bounds__(kManyThreads, 1)
+attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Kv4AttnArgs p) {
   using Cfg = ManyCfg<D>;
   constexpr int NR = Cfg::kRing;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -70,10 +82,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) attention_kv4_many_kernel(con
   const long long wb = wait_budget(p.wait_cycles);
   if (threadIdx.x == 0) {
     *abort_flag = 0;
-    mbar_init(q_full, 128);
+    mbar_init(q_full, kDecodeWarps);
     mbar_init(q_empty, 1);
     for (int s = 0; s < NR; ++s) {
-      mbar_init(ring_full(s), 128);
+      mbar_init(ring_full(s), CODES ? kDecodeWarps : 1);
       mbar_init(ring_empty(s), 1);
     }
     for (int t = 0; t < 2; ++t) {
@@ -122,165 +134,170 @@ __global__ void __launch_bounds__(kManyThreads, 1) attention_kv4_many_kernel(con
     x.nkv = min(per, blocks - x.kb0);
     return x;
   };
-  // Item i of a unit's stream of operand tiles: keys (v = 0) or values of which block.  A lone tile has two blocks under way.
+  // Tile i of a unit's stream: keys (v = 0) or values of which block.  A lone tile has two blocks under way.
   auto item_at = [](int i, int nkv, bool dual, int &j, int &v) {
     j = i >> 1, v = i & 1;                                // K 0, V 0, K 1, V 1, ...
     if (dual && nkv > 1) {                                // K 0, K 1, V 0, K 2, V 1, K 3, ... V nkv-2, V nkv-1
-      const int k = i - 2, alt = 2 * (nkv - 2);
-      v = k >= alt || (k >= 0 && (k & 1) == 0);
-      j = k < 0 ? i : k < alt ? (k >> 1) + (v ? 0 : 2) : k - alt + nkv - 2;
+      const bool last = i == 2 * nkv - 1;
+      v = last || (i > 0 && (i & 1) == 0);
+      j = last ? nkv - 1 : v ? (i >> 1) - 1 : (i + 1) >> 1;
     }
   };
   float m_ref = kNoRowMax, l_run = 0.f;       // softmax threads: running maximum and sum of this thread's query row and stream
   bool final_ok = true, any_block = false;    // softmax threads: the stream's last P V has completed; there was one
 
-  if (warp < kDecodeWarp) {
-    setmaxnreg_dec<kRegsMma>();
-    if (warp == 0) {
-      // ---------------------------------------------------------------- MMA issuer: the whole warp walks, one lane issues
-      constexpr uint32_t idesc_s = umma_idesc_bf16(kTileRows, kBlockKeys);
-      constexpr uint32_t idesc_o = umma_idesc_bf16(kTileRows, D) | (1u << 16);       // bit 16: the values are MN-major
-      const uint32_t leader = elect_one() ? 1u : 0u;
-      auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status, abort_flag, wb)) != 0; };
-      const uint64_t q_desc = smem_desc_sw128(q_smem), k_desc = smem_desc_sw128(ring_smem), v_desc = smem_desc_sw128_mn(ring_smem, kAtom);
-      auto issue_s = [&](int t, int qt, int slot) {       // S buffer t = Q_qt K^T
-        const uint64_t dq = q_desc + static_cast<uint32_t>(qt * (Cfg::kTileBytes >> 4)), dk = k_desc + static_cast<uint32_t>(slot * (Cfg::kTileBytes >> 4));
+  if (warp == 0) {
+    setmaxnreg_dec<kRegsDecode>();
+    // ---------------------------------------------------------------- MMA issuer: the whole warp walks, one lane issues
+    constexpr uint32_t idesc_s = umma_idesc_bf16(kTileRows, kBlockKeys);
+    constexpr uint32_t idesc_o = umma_idesc_bf16(kTileRows, D) | (1u << 16);       // bit 16: the values are MN-major
+    const uint32_t leader = elect_one() ? 1u : 0u;
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status, abort_flag, wb)) != 0; };
+    const uint64_t q_desc = smem_desc_sw128(q_smem), k_desc = smem_desc_sw128(ring_smem), v_desc = smem_desc_sw128_mn(ring_smem, kAtom);
+    auto issue_s = [&](int t, int qt, int slot) {       // S buffer t = Q_qt K^T
+      const uint64_t dq = q_desc + static_cast<uint32_t>(qt * (Cfg::kTileBytes >> 4)), dk = k_desc + static_cast<uint32_t>(slot * (Cfg::kTileBytes >> 4));
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          constexpr uint32_t a = kAtom >> 4;
-          umma_bf16_if(leader, tmem_base + t * kBlockKeys, dq + ((k / 4) * a + 2 * (k % 4)), dk + ((k / 4) * a + 2 * (k % 4)), idesc_s, k != 0);
-        }
-        umma_commit_if(leader, s_full(t));
-      };
-      auto issue_pv = [&](int t, int slot, int half, bool accumulate) {     // O_t (+)= P_t V over 64 keys
-        const uint64_t dv = v_desc + static_cast<uint32_t>(slot * (Cfg::kTileBytes >> 4) + half * (64 * 128 >> 4));
-        const uint32_t to = tmem_base + 256 + t * D, tp = tmem_base + t * kBlockKeys + half * 32;
+      for (int k = 0; k < D / 16; ++k) {
+        constexpr uint32_t a = kAtom >> 4;
+        umma_bf16_if(leader, tmem_base + t * kBlockKeys, dq + ((k / 4) * a + 2 * (k % 4)), dk + ((k / 4) * a + 2 * (k % 4)), idesc_s, k != 0);
+      }
+      umma_commit_if(leader, s_full(t));
+    };
+    auto issue_pv = [&](int t, int slot, int half, bool accumulate) {     // O_t (+)= P_t V over 64 keys
+      const uint64_t dv = v_desc + static_cast<uint32_t>(slot * (Cfg::kTileBytes >> 4) + half * (64 * 128 >> 4));
+      const uint32_t to = tmem_base + 256 + t * D, tp = tmem_base + t * kBlockKeys + half * 32;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) umma_bf16_tmem_a_if(leader, to, tp + 8 * k, dv + k * (16 * 128 >> 4), idesc_o, (accumulate || k != 0) ? 1u : 0u);
-      };
-      bool ok = true;
-      uint32_t q_par = 0, p_par = 0, phase = 0;           // p_par: a bit a stream
-      int slot = 0;
-      auto take = [&]() {                                 // the next tile of the ring; its slot
-        const int s = slot;
-        ok = ok && wait(ring_full(s), phase);
-        tc_fence_after();
-        if (++slot == NR) { slot = 0; phase ^= 1u; }
-        return s;
-      };
-      // P V of the next block of stream t over the values in slot `vs` (taken when first needed)
-      auto pv = [&](int t, int &vs, bool accumulate, bool last) {
-        ok = ok && wait(p_half(t), p_par >> t & 1u);
-        if (vs < 0) vs = take();
-        if (!ok) return;
-        tc_fence_after();
-        issue_pv(t, vs, 0, accumulate);
-        ok = wait(p_full(t), p_par >> t & 1u);
-        if (!ok) return;
-        p_par ^= 1u << t;
-        tc_fence_after();
-        issue_pv(t, vs, 1, true);
-        umma_commit_if(leader, last ? o_last(t) : o_full(t));
-      };
-      for (int u = unit0; ok && u < p.units; u += unit_step) {
-        const Unit x = unit_at(u);
-        const int nkv = x.nkv;
-        if (nkv == 0) continue;
-        ok = wait(q_full, q_par);
-        q_par ^= 1u;
-        if (!ok) break;
-        int ks = take();
-        if (!ok) break;
-        issue_s(0, 0, ks);
-        if (x.ntiles == 2) issue_s(1, 1, ks);
-        umma_commit_if(leader, ring_empty(ks));
-        if (nkv == 1) umma_commit_if(leader, q_empty);
-        if (x.ntiles == 2) {
-          for (int j = 0; ok && j < nkv; ++j) {
-            int vs = -1;
-            ks = -1;
-            for (int t = 0; ok && t < 2; ++t) {
-              pv(t, vs, j > 0, j + 1 == nkv);
+      for (int k = 0; k < 4; ++k) umma_bf16_tmem_a_if(leader, to, tp + 8 * k, dv + k * (16 * 128 >> 4), idesc_o, (accumulate || k != 0) ? 1u : 0u);
+    };
+    bool ok = true;
+    uint32_t q_par = 0, p_par = 0, phase = 0;           // p_par: a bit a stream
+    int slot = 0;
+    auto take = [&]() {                                 // the next tile of the ring; its slot
+      const int s = slot;
+      ok = ok && wait(ring_full(s), phase);
+      tc_fence_after();
+      if (++slot == NR) { slot = 0; phase ^= 1u; }
+      return s;
+    };
+    // P V of the next block of stream t over the values in slot `vs` (taken when first needed)
+    auto pv = [&](int t, int &vs, bool accumulate, bool last) {
+      ok = ok && wait(p_half(t), p_par >> t & 1u);
+      if (vs < 0) vs = take();
+      if (!ok) return;
+      tc_fence_after();
+      issue_pv(t, vs, 0, accumulate);
+      ok = wait(p_full(t), p_par >> t & 1u);
+      if (!ok) return;
+      p_par ^= 1u << t;
+      tc_fence_after();
+      issue_pv(t, vs, 1, true);
+      umma_commit_if(leader, last ? o_last(t) : o_full(t));
+    };
+    for (int u = unit0; ok && u < p.units; u += unit_step) {
+      const Unit x = unit_at(u);
+      const int nkv = x.nkv;
+      if (nkv == 0) continue;
+      ok = wait(q_full, q_par);
+      q_par ^= 1u;
+      if (!ok) break;
+      int ks = take();
+      if (!ok) break;
+      issue_s(0, 0, ks);
+      if (x.ntiles == 2) issue_s(1, 1, ks);
+      umma_commit_if(leader, ring_empty(ks));
+      if (nkv == 1) umma_commit_if(leader, q_empty);
+      if (x.ntiles == 2) {
+        for (int j = 0; ok && j < nkv; ++j) {
+          int vs = -1;
+          ks = -1;
+          for (int t = 0; ok && t < 2; ++t) {
+            pv(t, vs, j > 0, j + 1 == nkv);
+            if (!ok) break;
+            if (t == 1) umma_commit_if(leader, ring_empty(vs));
+            if (j + 1 < nkv) {
+              if (t == 0) ks = take();
               if (!ok) break;
-              if (t == 1) umma_commit_if(leader, ring_empty(vs));
-              if (j + 1 < nkv) {
-                if (t == 0) ks = take();
-                if (!ok) break;
-                issue_s(t, t, ks);
-                if (t == 1) {
-                  umma_commit_if(leader, ring_empty(ks));
-                  if (j + 2 == nkv) umma_commit_if(leader, q_empty);
-                }
+              issue_s(t, t, ks);
+              if (t == 1) {
+                umma_commit_if(leader, ring_empty(ks));
+                if (j + 2 == nkv) umma_commit_if(leader, q_empty);
               }
             }
           }
-        } else {
-          if (nkv > 1) {
+        }
+      } else {
+        if (nkv > 1) {
+          ks = take();
+          if (!ok) break;
+          issue_s(1, 0, ks);
+          umma_commit_if(leader, ring_empty(ks));
+          if (nkv == 2) umma_commit_if(leader, q_empty);
+        }
+        for (int j = 0; ok && j < nkv; ++j) {
+          const int t = j & 1;
+          int vs = -1;
+          pv(t, vs, j > 1, j + 2 >= nkv);
+          if (!ok) break;
+          umma_commit_if(leader, ring_empty(vs));
+          if (j + 2 < nkv) {
             ks = take();
             if (!ok) break;
-            issue_s(1, 0, ks);
+            issue_s(t, 0, ks);
             umma_commit_if(leader, ring_empty(ks));
-            if (nkv == 2) umma_commit_if(leader, q_empty);
-          }
-          for (int j = 0; ok && j < nkv; ++j) {
-            const int t = j & 1;
-            int vs = -1;
-            pv(t, vs, j > 1, j + 2 >= nkv);
-            if (!ok) break;
-            umma_commit_if(leader, ring_empty(vs));
-            if (j + 2 < nkv) {
-              ks = take();
-              if (!ok) break;
-              issue_s(t, 0, ks);
-              umma_commit_if(leader, ring_empty(ks));
-              if (j + 3 == nkv) umma_commit_if(leader, q_empty);
-            }
+            if (j + 3 == nkv) umma_commit_if(leader, q_empty);
           }
         }
       }
     }
   } else if (warp < kManySoftmaxWarp) {
-    // ------------------------------------------------------------------ decode
+    // ------------------------------------------------------------------ operand tiles
     setmaxnreg_dec<kRegsDecode>();
-    const int dt = static_cast<int>(threadIdx.x) - 32 * kDecodeWarp, dw = dt >> 5;
+    const int dw = warp - 1, dt = static_cast<int>(threadIdx.x) - 32;
     // A lane decodes 32 values (one group) of a row at a time, eight neighbouring lanes eight neighbouring rows: the stores of a
-    // quarter of a warp then fall into eight different 16-byte columns of the swizzled tile.
-    constexpr int kPieces = D / 32, kStep = 32 / kPieces, kReps = 32 / kStep;       // rows at a time, times for a warp's 32 rows
-    const int piece = (lane >> 3) % kPieces, lrow = dw * 32 + (lane & 7) + 8 * ((lane >> 3) / kPieces);
+    // quarter of a warp then fall into eight different 16-byte columns of the swizzled tile.  So a warp has kStep rows at a time; the
+    // kParts parts of a tile go round the seven warps, for the values from the other end.
+    constexpr int kPieces = D / 32, kStep = 32 / kPieces, kParts = kBlockKeys / kStep, kReps = (kParts + kDecodeWarps - 1) / kDecodeWarps;
+    const int piece = (lane >> 3) % kPieces, lrow = (lane & 7) + 8 * ((lane >> 3) / kPieces);
     struct Codes {
       uint4 w[kReps];
       uint32_t s[kReps];
     };
     bool ok = true;
     int slot = 0;
-    uint32_t phase = 0, q_units = 0;
+    uint32_t phase = 0, q_units = 0, armed = 0, armed_par = 0;        // slots that a copy was requested into, and the parity of the last
     for (int u = unit0; ok && u < p.units; u += unit_step) {
       const Unit x = unit_at(u);
       if (x.nkv == 0) continue;
       const bool dual = x.ntiles == 1;
-      const long long row0 = x.e * p.elem_stride + static_cast<long long>(x.h) * p.L_cap;
-      auto load = [&](int i, Codes &c) {
-        int j, v;
-        item_at(i, x.nkv, dual, j, v);
-        const int key0 = (x.kb0 + j) * kBlockKeys + lrow;
+      const long long row0 = x.e * p.elem_stride + static_cast<long long>(x.h) * p.L_cap + x.kb0 * kBlockKeys;
+      const int left = x.keys - x.kb0 * kBlockKeys;       // rows of the unit from the first block here
+      auto part_of = [&](int v, int k) { return k * kDecodeWarps + (v ? kDecodeWarps - 1 - dw : dw); };
+      auto load = [&](int v, int j, int k, Codes &c) {    // block j, part k of this warp
+        const int part = part_of(v, k), key = j * kBlockKeys + part * kStep + lrow;
+        const bool there = part < kParts && key < left && j < x.nkv;
         const uint8_t *codes = v ? p.v_codes : p.k_codes, *scales = v ? p.v_scales : p.k_scales;
-#pragma unroll
-        for (int k = 0; k < kReps; ++k) {
-          const int key = key0 + k * kStep;
-          const bool there = i < 2 * x.nkv && key < x.keys;
-          c.w[k] = there ? __ldg(reinterpret_cast<const uint4 *>(codes + (row0 + key) * (D / 2)) + piece) : make_uint4(0, 0, 0, 0);
-          c.s[k] = there ? __ldg(scales + (row0 + key) * (D / kKv4Group) + piece) : 0u;
-        }
+        c.w[k] = there ? __ldg(reinterpret_cast<const uint4 *>(codes + (row0 + key) * (D / 2)) + piece) : make_uint4(0, 0, 0, 0);
+        c.s[k] = there ? __ldg(scales + (row0 + key) * (D / kKv4Group) + piece) : 0u;
       };
-      auto put = [&](const Codes &c) {
-        if (!ok) return;
+      // Requests that bring block j to L2: a tile decoded is a tile's time until the next one is read, less than HBM takes.
+      auto fetch = [&](int v, int j) {
+        if (lane != 0 || dw != (v ? 0 : kDecodeWarps - 1) || j >= x.nkv) return;
+        const int n = min(kBlockKeys, ((left + 7) & ~7) - j * kBlockKeys);            // whole 16 bytes of scales; within the cache (L_cap % 8 == 0)
+        const long long at = row0 + j * kBlockKeys;
+        l2_fetch((v ? p.v_codes : p.k_codes) + at * (D / 2), n * (D / 2));
+        l2_fetch((v ? p.v_scales : p.k_scales) + at * (D / kKv4Group), n * (D / kKv4Group));
+      };
+      auto put = [&](int v, int j, Codes &c) {
         ok = __all_sync(0xffffffffu, mbar_wait(ring_empty(slot), phase ^ 1u, p.status, abort_flag, wb));
         if (!ok) return;
+        fetch(v, j + kFetchAhead);
         const uint32_t tile = ring_smem + slot * Cfg::kTileBytes + (piece >> 1) * kAtom;
 #pragma unroll
         for (int k = 0; k < kReps; ++k) {
-          const int row = lrow + k * kStep;
+          if (part_of(v, k) >= kParts) continue;
+          const int row = part_of(v, k) * kStep + lrow;
           const uint32_t s2 = kv4_scale2(c.s[k]), f2 = kv4_offset2(s2), w[4] = {c.w[k].x, c.w[k].y, c.w[k].z, c.w[k].w};
+          load(v, j + 1, k, c);                           // the next block's, into the registers that have just been read
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
             uint32_t o[4];
@@ -290,32 +307,72 @@ __global__ void __launch_bounds__(kManyThreads, 1) attention_kv4_many_kernel(con
           }
         }
         fence_proxy_async_smem();
-        mbar_arrive(ring_full(slot));
-        if (++slot == NR) { slot = 0; phase ^= 1u; }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ring_full(slot));
       };
-      Codes a, b;
-      load(0, a);
-      load(1, b);
+      Codes ck, cv;
+      if constexpr (CODES) {
+        for (int j = 1; j < kFetchAhead; ++j) fetch(0, j), fetch(1, j);
+#pragma unroll
+        for (int k = 0; k < kReps; ++k) load(0, 0, k, ck);
+#pragma unroll
+        for (int k = 0; k < kReps; ++k) load(1, 0, k, cv);
+      }
       if (q_units > 0) ok = __all_sync(0xffffffffu, mbar_wait(q_empty, (q_units - 1) & 1u, p.status, abort_flag, wb));
       if (!ok) break;
       ++q_units;
-      constexpr int kLanes = D / 8;                       // lanes of a query row
-      for (int k = dt; k < x.ntiles * kTileRows * kLanes; k += 128) {
-        const int row = k / kLanes, ch = k % kLanes, rho = x.rho0 + row;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (rho < nrows) v = __ldg(reinterpret_cast<const uint4 *>(p.q + (static_cast<long long>(x.e) * p.r + rho / G) * p.ldq + (x.h * G + rho % G) * D) + ch);
+      constexpr int kLanes = D / 8;                       // 16-byte pieces of a query row; rows that are not there become zeros
+      for (int n = dt; n < x.ntiles * kTileRows * kLanes; n += 32 * kDecodeWarps) {
+        const int row = n / kLanes, ch = n % kLanes, rho = x.rho0 + row;
+        const bool there = rho < nrows;
+        const bf16 *src = p.q + (there ? (static_cast<long long>(x.e) * p.r + rho / G) * p.ldq + (x.h * G + rho % G) * D + ch * 8 : 0);
         const uint32_t dst = q_smem + (row >> 7) * Cfg::kTileBytes + (ch >> 3) * kAtom + (row & 127) * 128 + ((ch ^ row) & 7) * 16;
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
       }
-      fence_proxy_async_smem();
-      mbar_arrive(q_full);
-      for (int i = 0; ok && i < 2 * x.nkv; i += 2) {
-        put(a);
-        load(i + 2, a);
-        put(b);
-        load(i + 3, b);
+      // The first tile is decoded while the queries are on the way.
+      if constexpr (CODES) {
+        for (int i = 0; ok && i < 2 * x.nkv; ++i) {
+          int j, v;
+          item_at(i, x.nkv, dual, j, v);
+          if (v) put(1, j, cv);
+          else put(0, j, ck);
+          if (i == 0) {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full);
+          }
+          if (++slot == NR) { slot = 0; phase ^= 1u; }
+        }
+      } else {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full);
+        if (threadIdx.x == 32) {
+          for (int i = 0; ok && i < 2 * x.nkv; ++i) {
+            int j, v;
+            item_at(i, x.nkv, dual, j, v);
+            ok = mbar_wait(ring_empty(slot), phase ^ 1u, p.status, abort_flag, wb);
+            if (!ok) break;
+            mbar_expect_tx(ring_full(slot), Cfg::kTileBytes);
+#pragma unroll
+            for (int a = 0; a < D / 64; ++a)
+              tma_load_3d(ring_smem + slot * Cfg::kTileBytes + a * kAtom, v ? &tmV : &tmK, ring_full(slot), a * 64, (x.kb0 + j) * kBlockKeys, x.e * p.Hkv + x.h);
+            armed |= 1u << slot;
+            armed_par = (armed_par & ~(1u << slot)) | (phase << slot);
+            if (++slot == NR) { slot = 0; phase ^= 1u; }
+          }
+        }
+        ok = __all_sync(0xffffffffu, ok) != 0;            // the lane that requests may have given up: its warp goes on together or not at all
       }
     }
+    if (!CODES && threadIdx.x == 32 && !ok)               // let every copy that was requested land before the shared memory is released
+      for (int s = 0; s < NR; ++s)
+        if (armed >> s & 1u) {
+          const long long t0 = clock64();
+          while (!mbar_try_wait(ring_full(s), armed_par >> s & 1u) && clock64() - t0 < kWaitCycles) {}
+        }
   } else {
     // ------------------------------------------------------------------ softmax
     setmaxnreg_inc<kRegsRows>();
@@ -584,28 +641,34 @@ __global__ void __launch_bounds__(kManyThreads, 1) attention_kv4_many_kernel(con
   }
 }
 
-template <int D, bool RANGES>
+template <int D, bool RANGES, bool CODES>
 static cudaError_t many_prepare(int dev) {
   static unsigned long long prepared = 0;                 // a bit a device
   if (dev < 64 && (prepared >> dev & 1)) return cudaSuccess;
   // The register split draws on what the block was launched with: refuse a build whose kernel got fewer.
   cudaFuncAttributes fa;
-  cudaError_t e = cudaFuncGetAttributes(&fa, attention_kv4_many_kernel<D, RANGES>);
+  cudaError_t e = cudaFuncGetAttributes(&fa, attention_kv4_many_kernel<D, RANGES, CODES>);
   if (e != cudaSuccess) return e;
-  if (kManyThreads * fa.numRegs < 128 * (kRegsMma + kRegsDecode + 2 * kRegsRows)) return cudaErrorInvalidConfiguration;
-  e = cudaFuncSetAttribute(attention_kv4_many_kernel<D, RANGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<D>::kSmemBytes);
+  if (fa.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
+  e = cudaFuncSetAttribute(attention_kv4_many_kernel<D, RANGES, CODES>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<D>::kSmemBytes);
   if (e == cudaSuccess && dev < 64) prepared |= 1ull << dev;
   return e;
 }
 
-int g_many_tiles = 0, g_many_splits = 0;
+int g_many_tiles = 0, g_many_splits = 0, g_many_pass = 0;
+
+size_t attention_kv4_workspace(int B, int Hkv, int G, int r, int D, int L) {
+  if (g_many_pass ? g_many_pass < 0 : static_cast<long long>(r) * G <= 512) return 0;
+  return static_cast<size_t>(B) * Hkv * L * D * 4;
+}
 
 template <int D>
-static cudaError_t launch_many_d(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
+static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  const long long rows = static_cast<long long>(a.r) * (a.H / a.Hkv);
+  const int G = a.H / a.Hkv;
+  const long long rows = static_cast<long long>(a.r) * G;
   if (rows > INT_MAX - 256) return cudaErrorInvalidValue;
   a.tiles_per_cta = g_many_tiles ? g_many_tiles : rows > kTileRows ? 2 : 1;
   a.kv_splits = g_many_splits ? g_many_splits : 1;
@@ -614,12 +677,33 @@ static cudaError_t launch_many_d(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
   a.units = static_cast<int>(units);
   a.div_nqt = make_fast_div(static_cast<unsigned>(nqt), units);
   a.div_h = make_fast_div(a.Hkv, units);
-  if (a.kv_splits <= 1) {
-    e = many_prepare<D, false>(dev);
+  CUtensorMap tk = {}, tv = {};
+  const size_t need = attention_kv4_workspace(a.B, a.Hkv, G, a.r, D, a.L);
+  if (a.L > 0 && need > 0 && workspace && bytes >= need) {
+    Kv4Args x = {};
+    x.k_out = static_cast<bf16 *>(workspace);
+    x.v_out = x.k_out + static_cast<size_t>(a.B) * a.Hkv * a.L * D;
+    x.k_codes = const_cast<uint8_t *>(a.k_codes); x.v_codes = const_cast<uint8_t *>(a.v_codes);
+    x.k_scales = const_cast<uint8_t *>(a.k_scales); x.v_scales = const_cast<uint8_t *>(a.v_scales);
+    x.elem_stride = a.elem_stride;
+    x.B = a.B; x.H = a.Hkv; x.D = D; x.L_cap = a.L_cap; x.n = a.L;
+    x.out_row = D; x.out_head = static_cast<long long>(a.L) * D; x.out_elem = x.out_head * a.Hkv;
+    x.status = a.status;
+    const uint64_t heads = static_cast<uint64_t>(a.B) * a.Hkv;
+    if (!tmap_3d(&tk, x.k_out, D, a.L, heads, D, static_cast<uint64_t>(a.L) * D, 64, 128) ||
+        !tmap_3d(&tv, x.v_out, D, a.L, heads, D, static_cast<uint64_t>(a.L) * D, 64, 128))
+      return cudaErrorInvalidValue;
+    e = launch_kv4_rows(false, x, st);
+    if (e == cudaSuccess) e = many_prepare<D, false, false>(dev);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attention_kv4_many_kernel<D, false>, dim3(a.units < num_sms ? a.units : num_sms), dim3(kManyThreads), ManyCfg<D>::kSmemBytes, st, a);
+    return launch_pdl(attention_kv4_many_kernel<D, false, false>, dim3(a.units < num_sms ? a.units : num_sms), dim3(kManyThreads), ManyCfg<D>::kSmemBytes, st, tk, tv, a);
   }
-  e = many_prepare<D, true>(dev);
+  if (a.kv_splits <= 1) {
+    e = many_prepare<D, false, true>(dev);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(attention_kv4_many_kernel<D, false, true>, dim3(a.units < num_sms ? a.units : num_sms), dim3(kManyThreads), ManyCfg<D>::kSmemBytes, st, tk, tv, a);
+  }
+  e = many_prepare<D, true, true>(dev);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.units * a.kv_splits);
@@ -634,11 +718,11 @@ static cudaError_t launch_many_d(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
   attr[1] = pdl_attribute();
   cfg.attrs = attr;
   cfg.numAttrs = one_predecessor(st) ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, attention_kv4_many_kernel<D, true>, a);
+  return cudaLaunchKernelEx(&cfg, attention_kv4_many_kernel<D, true, true>, tk, tv, a);
 }
 
-cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, int num_sms, cudaStream_t st) {
-  return a.D == 64 ? launch_many_d<64>(a, num_sms, st) : launch_many_d<128>(a, num_sms, st);
+cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {
+  return a.D == 64 ? launch_many_d<64>(a, workspace, bytes, num_sms, st) : launch_many_d<128>(a, workspace, bytes, num_sms, st);
 }
 
 }  // namespace fvar

@@ -1766,15 +1766,21 @@ fvar_status fvar_kv4_read(const fvar_kv4 *cache, int n, int L0, const int *start
   if (off_grid(K_out, 16) || off_grid(V_out, 16)) return kfail(FVAR_EINVAL, "kv4_read: K_out and V_out must be 16-byte aligned");
   Kv4Args a = {};
   a.k_out = static_cast<bf16 *>(K_out); a.v_out = static_cast<bf16 *>(V_out);
+  a.out_head = cache->head_dim; a.out_row = a.out_head * cache->n_heads; a.out_elem = a.out_row * n;
   return kv4_rows(false, cache, a, n, L0, start, count, stream);
 }
 
+size_t fvar_attention_kv4_workspace(const fvar_kv4 *cache, int H, int r, int L) {
+  if (kv4_wrong(cache) || H <= 0 || H % cache->n_heads || r <= 0 || L <= 0 || L > cache->L_cap) return 0;
+  return attention_kv4_workspace(cache->B, cache->n_heads, H / cache->n_heads, r, cache->head_dim, L);
+}
+
 fvar_status fvar_attention_kv4(const void *q, long long ldq, const fvar_kv4 *cache, int H, int r, int L, const int *limits, void *out,
-                               void *stream) {
+                               void *workspace, size_t workspace_bytes, void *stream) {
   if (const char *why = kv4_wrong(cache)) return kfail(FVAR_EINVAL, why);
   if (!q || !out || H <= 0 || H % cache->n_heads || r <= 0 || L < 0 || L > cache->L_cap || ldq % 8 || ldq < static_cast<long long>(H) * cache->head_dim)
     return kfail(FVAR_EINVAL, "attention_kv4: bad arguments");
-  if (off_grid(q, 16) || off_grid(out, 16)) return kfail(FVAR_EINVAL, "attention_kv4: q and out must be 16-byte aligned");
+  if (off_grid(q, 16) || off_grid(out, 16) || off_grid(workspace, 16)) return kfail(FVAR_EINVAL, "attention_kv4: q, out and workspace must be 16-byte aligned");
   Kv4AttnArgs a = {};
   kv4_fields(cache, a);
   a.q = static_cast<const bf16 *>(q); a.ldq = ldq; a.H = H; a.Hkv = cache->n_heads; a.r = r; a.L = L; a.limits = limits;
@@ -1785,7 +1791,7 @@ fvar_status fvar_attention_kv4(const void *q, long long ldq, const fvar_kv4 *cac
   int dev = 0, sms = 0;
   FK_CUDA(cudaGetDevice(&dev), "get device");
   FK_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev), "device attribute");
-  FK_CUDA(launch_attention_kv4(a, sms, static_cast<cudaStream_t>(stream)), "attention_kv4");
+  FK_CUDA(launch_attention_kv4(a, workspace, workspace_bytes, sms, static_cast<cudaStream_t>(stream)), "attention_kv4");
   return FVAR_OK;
 }
 

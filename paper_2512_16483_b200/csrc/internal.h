@@ -297,7 +297,8 @@ cudaError_t launch_split_rows(const float *x, long long x_off, long long x_strid
 // Cache in 4 bits (kv4.cu, attention_kv4.cu; format in include/fvar.h).
 struct Kv4Args {
   const bf16 *k_rows, *v_rows;            // write: row (b, i) at (b * n + i) * ld
-  bf16 *k_out, *v_out;                    // read: [B][n][H * D]
+  bf16 *k_out, *v_out;                    // read: row i of head h of element b at b * out_elem + i * out_row + h * out_head
+  long long out_elem, out_row, out_head;
   uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
   long long ld, elem_stride;              // elem_stride: cache rows from one element to the next
   int B, H, D, L_cap, n, L0;
@@ -321,8 +322,10 @@ struct Kv4AttnArgs {
   FastDiv div_nqt, div_h;
 };
 // More than 16 query rows a cache head: tcgen05 (attention_kv4_many.cu).
-cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, int num_sms, cudaStream_t st);
-cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, int num_sms, cudaStream_t st);
+cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st);
+// Bytes of workspace that such a call can use (0: none).
+size_t attention_kv4_workspace(int B, int Hkv, int G, int r, int D, int L);
+cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st);
 
 // Self-test of the bounded wait: one CTA waits on an mbarrier nobody signals with a budget of `cycles`, flags the
 // status word and returns.

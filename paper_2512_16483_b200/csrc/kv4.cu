@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kKv4Threads) kv4_read_kernel(const __grid_cons
       const uint32_t s2 = kv4_scale2(byte[v][t]);
       uint32_t o[4];
       kv4_word(word[v][t], s2, kv4_offset2(s2), o);
-      bf16 *dst = (v ? p.v_out : p.k_out) + ((static_cast<long long>(w.b) * p.n + w.i0 + t * kStep + r0) * p.H + w.h) * D + c * 8;
+      bf16 *dst = (v ? p.v_out : p.k_out) + w.b * p.out_elem + (w.i0 + t * kStep + r0) * p.out_row + w.h * p.out_head + c * 8;
       __stcs(reinterpret_cast<uint4 *>(dst), make_uint4(o[0], o[1], o[2], o[3]));
     }
 }

@@ -191,8 +191,120 @@ PyObject *scale_transition(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---- the cache in 4 bits.  The first two arguments are the address of the binding's fvar_kv4 and the device its arrays are on.
+struct Kv4Call {
+  const fvar_kv4 *c = nullptr;
+  int dev = -1;
+};
+// The cache of the call if its arrays are on the current device.
+bool as_cache(PyObject *addr, PyObject *dev, Kv4Call *k) {
+  if (!PyLong_CheckExact(addr) || !as_int(dev, &k->dev) || k->dev != c10::cuda::current_device()) return false;
+  k->c = static_cast<const fvar_kv4 *>(PyLong_AsVoidPtr(addr));
+  return k->c != nullptr;
+}
+bool here(const at::Tensor &t, const Kv4Call &k) { return t.device().index() == k.dev; }
+// bf16 rows [B][n][C] at equal distances *ld (see _rows_of in binding.py).
+const at::Tensor *as_rows(PyObject *o, const Kv4Call &k, int64_t *ld) {
+  const at::Tensor *t = plain(o);
+  if (!t || t->scalar_type() != at::kBFloat16 || t->dim() != 3 || !here(*t, k) || !fits(t->size(1)) || !fits(t->size(2))) return nullptr;
+  const int64_t B = t->size(0), n = t->size(1), C = t->size(2);
+  *ld = n > 1 ? t->stride(1) : B > 1 ? t->stride(0) : C;
+  if (B != k.c->B || (t->stride(2) != 1 && C != 1) || (B > 1 && n > 0 && t->stride(0) != n * *ld)) return nullptr;
+  return t;
+}
+// int32 of the given size, or None (null).
+bool as_ints(PyObject *o, const Kv4Call &k, int64_t rows, int64_t cols, const int **p) {
+  *p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor *t = plain(o, at::kInt, cols > 0 ? 2 : 1);
+  if (!t || !here(*t, k) || t->size(0) != rows || (cols > 0 && t->size(1) != cols)) return false;
+  *p = static_cast<const int *>(t->data_ptr());
+  return true;
+}
+// start: an int, or int32 [B].
+bool as_start(PyObject *o, const Kv4Call &k, int *L0, const int **p) {
+  *p = nullptr;
+  *L0 = 0;
+  return PyLong_CheckExact(o) ? as_int(o, L0) : o != Py_None && as_ints(o, k, k.c->B, 0, p);
+}
+int64_t kv4_width(const Kv4Call &k) { return static_cast<int64_t>(k.c->n_heads) * k.c->head_dim; }
+
+// (cache, device, K, V, start, count) -> True
+PyObject *kv4_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject * {
+    Kv4Call k;
+    int64_t ld = 0, ldv = 0;
+    int L0 = 0;
+    const int *start = nullptr, *count = nullptr;
+    if (n != 6 || !as_cache(a[0], a[1], &k)) return none();
+    const at::Tensor *K = as_rows(a[2], k, &ld), *V = K ? as_rows(a[3], k, &ldv) : nullptr;
+    if (!V || ld != ldv || K->sizes() != V->sizes() || K->size(2) != kv4_width(k) || !as_start(a[4], k, &L0, &start) || !as_ints(a[5], k, k.c->B, 0, &count))
+      return none();
+    const void *kp = K->data_ptr(), *vp = V->data_ptr();
+    const int rows = static_cast<int>(K->size(1));
+    void *st = stream();
+    const fvar_status e = unlocked([&] { return fvar_kv4_write(k.c, kp, vp, ld, rows, L0, start, count, st); });
+    if (e != FVAR_OK) return PyLong_FromLong(e);
+    Py_RETURN_TRUE;
+  });
+}
+
+// (cache, device, n, start, count, (K, V)) -> True
+PyObject *kv4_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject * {
+    Kv4Call k;
+    int rows = 0, L0 = 0;
+    const int *start = nullptr, *count = nullptr;
+    if (n != 6 || !as_cache(a[0], a[1], &k) || !as_int(a[2], &rows) || rows < 0 || !as_start(a[3], k, &L0, &start) || !as_ints(a[4], k, k.c->B, 0, &count) ||
+        !PyTuple_CheckExact(a[5]) || PyTuple_GET_SIZE(a[5]) != 2)
+      return none();
+    const at::Tensor *o[2];
+    for (int i = 0; i < 2; ++i) {
+      o[i] = plain(PyTuple_GET_ITEM(a[5], i), at::kBFloat16, 3);
+      if (!o[i] || !here(*o[i], k) || o[i]->size(0) != k.c->B || o[i]->size(1) != rows || o[i]->size(2) != kv4_width(k)) return none();
+    }
+    void *kp = o[0]->data_ptr(), *vp = o[1]->data_ptr(), *st = stream();
+    const fvar_status e = unlocked([&] { return fvar_kv4_read(k.c, rows, L0, start, count, kp, vp, st); });
+    if (e != FVAR_OK) return PyLong_FromLong(e);
+    Py_RETURN_TRUE;
+  });
+}
+
+// (cache, device, q, L, limits, out) -> out, which is made when it is None
+PyObject *attention_kv4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject * {
+    Kv4Call k;
+    int64_t ld = 0;
+    int L = 0;
+    const int *limits = nullptr;
+    if (n != 6 || !as_cache(a[0], a[1], &k)) return none();
+    const at::Tensor *q = as_rows(a[2], k, &ld);
+    if (!q || k.c->head_dim <= 0 || q->size(2) % k.c->head_dim || !as_int(a[3], &L) || !as_ints(a[4], k, q->size(0), q->size(1), &limits)) return none();
+    const int r = static_cast<int>(q->size(1)), H = static_cast<int>(q->size(2) / k.c->head_dim);
+    at::Tensor fresh;
+    const at::Tensor *out = &fresh;
+    if (a[5] == Py_None) {
+      fresh = empty_like_device(*q, {q->size(0), q->size(1), q->size(2)}, at::kBFloat16);
+    } else {
+      out = plain(a[5], at::kBFloat16, 3);
+      if (!out || !here(*out, k) || out->sizes() != q->sizes()) return none();
+    }
+    const size_t bytes = fvar_attention_kv4_workspace(k.c, H, r, L);
+    at::Tensor work;
+    if (bytes) work = empty_like_device(*q, {static_cast<int64_t>(bytes)}, at::kByte);
+    const void *qp = q->data_ptr();
+    void *op = out->data_ptr(), *wp = bytes ? work.data_ptr() : nullptr, *st = stream();
+    const fvar_status e = unlocked([&] { return fvar_attention_kv4(qp, ld, k.c, H, r, L, limits, op, wp, bytes, st); });
+    if (e != FVAR_OK) return PyLong_FromLong(e);
+    if (a[5] == Py_None) return wrap(fresh);
+    Py_INCREF(a[5]);
+    return a[5];
+  });
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FAST(row_scores), FAST(select_topr), FAST(ln_modulate), FAST(rtr_fill), FAST(cfg_combine), FAST(scale_transition), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {FAST(row_scores), FAST(select_topr), FAST(ln_modulate), FAST(rtr_fill), FAST(cfg_combine), FAST(scale_transition), FAST(kv4_write), FAST(kv4_read), FAST(attention_kv4),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -49,7 +49,7 @@ BAD_CACHES = [{"k_codes": None}, {"v_codes": None}, {"k_scales": None}, {"v_scal
               {"k_scales": P + 2}, {"v_scales": P + 1}, {"B": 0}, {"n_heads": 0}, {"head_dim": 32}, {"head_dim": 96}, {"L_cap": 36}, {"L_cap": 0},
               {"elem_stride": 152}, {"elem_stride": 161}, {"elem_stride": -160}]
 GOOD = {"fvar_kv4_write": (P, P, 256, 3, 0, None, None, None), "fvar_kv4_read": (3, 0, None, None, P, P, None),
-        "fvar_attention_kv4": (P, 512, None, 8, 3, 40, None, P, None)}
+        "fvar_attention_kv4": (P, 512, None, 8, 3, 40, None, P, P, 0, None)}
 
 
 def _call(name, args, cache):
@@ -74,7 +74,7 @@ def test_bad_caches_are_refused(name):
 @pytest.mark.parametrize("name,vary", [
     ("fvar_kv4_write", {0: (None, P + 8), 1: (None, P + 4), 2: (248, 260, 0), 3: (-1, 41), 4: (-1, 38)}),
     ("fvar_kv4_read", {0: (-1, 41), 1: (-1, 38), 4: (None, P + 8), 5: (None, P + 2)}),
-    ("fvar_attention_kv4", {0: (None, P + 8), 1: (504, 516), 3: (0, -4, 6), 4: (0, -1), 5: (-1, 41), 7: (None, P + 8)}),
+    ("fvar_attention_kv4", {0: (None, P + 8), 1: (504, 516), 3: (0, -4, 6), 4: (0, -1), 5: (-1, 41), 7: (None, P + 8), 8: (P + 8,)}),
 ])
 def test_bad_arguments_are_refused(name, vary):
     from paper_2512_16483_b200 import binding
