@@ -304,7 +304,8 @@ struct Kv4Args {
   int B, H, D, L_cap, n, L0;
   const int *start, *count;
   unsigned *status;
-  long long units;                        // warps' work, filled by launch_kv4_rows
+  int units;                              // warps' work in an element, filled by launch_kv4_rows
+  FastDiv div_h;
 };
 cudaError_t launch_kv4_rows(bool write, Kv4Args a, cudaStream_t st);
 struct Kv4AttnArgs {

@@ -5,6 +5,7 @@
 // at once, all loads first; consecutive warps take consecutive heads of the same rows, which lie side by side in the input.
 #include "kv4.cuh"
 #include "ptx.cuh"
+#include "softmax.cuh"
 
 namespace fvar {
 
@@ -18,12 +19,13 @@ __device__ __forceinline__ uint32_t kv4_scale_byte(float top) {
   const int u = static_cast<int>((__float_as_uint(t) + 0x000FFFFFu) >> 20) - (107 << 3);      // exponent and three bits of mantissa
   return static_cast<uint32_t>(min(max(u, 0), 255));
 }
-// u = 8 + sign(x) min(7, floor(|x| / s + 1/2)).  |x| / s is a half-integer or at least 2^-9 away from one, so 2^-12 more than the
-// half makes up for the rounding of 1 / s and of the product.  NaN: fminf and the comparison leave 0 of it (see below).
+// x / s rounded to the nearest integer, halves away from zero, and kept within +-7: the sum with 1.5 2^23 + 8 has u = 8 + that in its
+// last four bits.  |x| / s is a half-integer or at least 2^-9 away from one (x has eight bits, s four), so 1 / s taken larger by 2^-13
+// moves the halves, and nothing else, across; it also covers the rounding of 1 / s and of the product.
+constexpr float kCodeBase = 12582920.0f;                  // 1.5 2^23 + 8
+constexpr uint32_t kCodeBits = 0x4B400000u;               // its bits, less 8
 __device__ __forceinline__ uint32_t kv4_code(float x, float inv_s) {
-  const float q = floorf(fmaf(fabsf(x), inv_s, 0.5f + 1.0f / 4096.0f));
-  const int m = static_cast<int>(fminf(q, 7.0f));
-  return static_cast<uint32_t>(x < 0.f ? 8 - m : 8 + m);
+  return __float_as_uint(fminf(fmaxf(fmaf(x, inv_s, kCodeBase), kCodeBase - 7.f), kCodeBase + 7.f));
 }
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
@@ -33,94 +35,105 @@ __device__ __forceinline__ uint32_t drop_nan2(uint32_t v) {
   return lo | hi;
 }
 
+// The rows of one warp: kRows rows from i0 on of head h of element b.
 struct Kv4Place {
-  int b, h, i0;                 // element, head, first row of the warp
-  int n;                        // rows of the element
+  int b, h, i0;
+  int n;                        // rows of the element that there are
   int at;                       // cache row of row 0
+  long long row0;               // row 0 of the head, in rows of the whole cache
 };
 template <int D>
-__device__ __forceinline__ bool kv4_place(const Kv4Args &p, Kv4Place &w) {
+__device__ __forceinline__ bool kv4_place(const Kv4Args &p, int b, Kv4Place &w) {
   constexpr int kRows = kPasses * (32 / (D / 8));
-  const long long unit = static_cast<long long>(blockIdx.x) * (kKv4Threads / 32) + (threadIdx.x >> 5);
+  const int unit = static_cast<int>(blockIdx.x) * (kKv4Threads / 32) + (threadIdx.x >> 5);
   if (unit >= p.units) return false;
-  const int blocks = (p.n + kRows - 1) / kRows;
-  w.h = static_cast<int>(unit % p.H);
-  const long long rest = unit / p.H;
-  w.b = static_cast<int>(rest / blocks);
-  w.i0 = static_cast<int>(rest - static_cast<long long>(w.b) * blocks) * kRows;
-  w.n = p.count ? min(max(p.count[w.b], 0), p.n) : p.n;
-  w.at = p.start ? p.start[w.b] : p.L0;
-  return true;
+  const int block = fast_div(unit, p.div_h);
+  w.h = unit - block * p.H;
+  w.i0 = block * kRows;
+  w.b = b;
+  w.n = p.count ? min(max(p.count[b], 0), p.n) : p.n;
+  w.at = p.start ? p.start[b] : p.L0;
+  w.row0 = b * p.elem_stride + static_cast<long long>(w.h) * p.L_cap;
+  return w.i0 < w.n;
 }
 // Cache row of row i of the element, -1 if there is none.
-__device__ __forceinline__ long long kv4_row(const Kv4Args &p, const Kv4Place &w, int i, bool &bad) {
+__device__ __forceinline__ int kv4_row(const Kv4Args &p, const Kv4Place &w, int i, bool &bad) {
   if (i >= w.n) return -1;
   const long long pos = static_cast<long long>(w.at) + i;
   if (pos < 0 || pos >= p.L_cap) { bad = true; return -1; }
-  return w.b * p.elem_stride + static_cast<long long>(w.h) * p.L_cap + pos;
+  return static_cast<int>(pos);
 }
 
 template <int D>
-__global__ void __launch_bounds__(kKv4Threads) kv4_write_kernel(const __grid_constant__ Kv4Args p) {
-  constexpr int kLanes = D / 8, kStep = 32 / kLanes;
-  pdl_wait();
-  pdl_launch_dependents();
-  Kv4Place w;
-  if (!kv4_place<D>(p, w)) return;
-  const int lane = threadIdx.x & 31, c = lane % kLanes, r0 = lane / kLanes;
+__device__ __forceinline__ void kv4_write_rows(const Kv4Args &p, const Kv4Place &w, int lane) {
+  constexpr int kLanes = D / 8, kStep = 32 / kLanes, kGroups = D / kKv4Group;
+  const int c = lane % kLanes, r0 = lane / kLanes;
   bool bad = false;
   uint4 x[2][kPasses];
-  long long row[kPasses];
+  int row[kPasses];
+  const long long src = (static_cast<long long>(w.b) * p.n + w.i0 + r0) * p.ld + w.h * D + c * 8;
 #pragma unroll
   for (int t = 0; t < kPasses; ++t) {
-    const int i = w.i0 + t * kStep + r0;
-    row[t] = kv4_row(p, w, i, bad);
-    const long long src = (static_cast<long long>(w.b) * p.n + i) * p.ld + w.h * D + c * 8;
+    row[t] = kv4_row(p, w, w.i0 + t * kStep + r0, bad);
 #pragma unroll
     for (int v = 0; v < 2; ++v)
-      x[v][t] = row[t] >= 0 ? __ldcs(reinterpret_cast<const uint4 *>((v ? p.v_rows : p.k_rows) + src)) : make_uint4(0, 0, 0, 0);
+      x[v][t] = row[t] >= 0 ? __ldcs(reinterpret_cast<const uint4 *>((v ? p.v_rows : p.k_rows) + src + t * kStep * p.ld)) : make_uint4(0, 0, 0, 0);
   }
   if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, kStatusBadIndex);
+  // the row whose scales this lane writes: a row's are kGroups bytes
+  const int srow = lane < kPasses * kStep ? kv4_row(p, w, w.i0 + lane, bad) : -1;
 #pragma unroll
-  for (int t = 0; t < kPasses; ++t)
+  for (int v = 0; v < 2; ++v) {
+    uint32_t bytes = 0;                                   // of the lane's group, a byte a pass
+    uint32_t *codes = reinterpret_cast<uint32_t *>(v ? p.v_codes : p.k_codes) + w.row0 * kLanes + c;
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
+    for (int t = 0; t < kPasses; ++t) {
       uint32_t e[4] = {x[v][t].x, x[v][t].y, x[v][t].z, x[v][t].w};
-      uint32_t top2 = 0;                                             // maxima of the bit patterns: ordered as the magnitudes are
+      // maxima of the bit patterns: ordered as the magnitudes are
+      uint32_t top2 = __vmaxu2(__vmaxu2(e[0] & 0x7FFF7FFFu, e[1] & 0x7FFF7FFFu), __vmaxu2(e[2] & 0x7FFF7FFFu, e[3] & 0x7FFF7FFFu));
+      if (__any_sync(0xffffffffu, (top2 & 0xFFFFu) > 0x7F80u || top2 > 0x7F80FFFFu)) {       // a NaN in the warp: rarely
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        e[k] = drop_nan2(e[k]);
-        top2 = __vmaxu2(top2, e[k] & 0x7FFF7FFFu);
+        for (int k = 0; k < 4; ++k) e[k] = drop_nan2(e[k]);
+        top2 = __vmaxu2(__vmaxu2(e[0] & 0x7FFF7FFFu, e[1] & 0x7FFF7FFFu), __vmaxu2(e[2] & 0x7FFF7FFFu, e[3] & 0x7FFF7FFFu));
       }
       top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 1));
       top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 2));
       const uint32_t byte = kv4_scale_byte(fmaxf(bf_lo(top2), bf_hi(top2)));
-      const float inv_s = __frcp_rn(__uint_as_float((byte + (107u << 3)) << 20));
-      uint32_t word = 0;
+      const float inv_s = __frcp_rn(__uint_as_float((byte + (107u << 3)) << 20)) * (1.0f + 1.0f / 8192.0f);
+      bytes |= byte << (8 * t);
+      uint32_t word = 0;                                  // modulo 2^32: what stands above the last four bits of a code is taken off as one
 #pragma unroll
-      for (int k = 0; k < 4; ++k) word |= kv4_code(bf_lo(e[k]), inv_s) << (4 * k) | kv4_code(bf_hi(e[k]), inv_s) << (16 + 4 * k);
-      if (row[t] >= 0) {
-        reinterpret_cast<uint32_t *>(v ? p.v_codes : p.k_codes)[row[t] * kLanes + c] = word;
-        if ((c & 3) == 0) (v ? p.v_scales : p.k_scales)[row[t] * (D / kKv4Group) + c / 4] = static_cast<uint8_t>(byte);
-      }
+      for (int k = 0; k < 4; ++k) word += (kv4_code(bf_lo(e[k]), inv_s) << (4 * k)) + (kv4_code(bf_hi(e[k]), inv_s) << (16 + 4 * k));
+      word -= kCodeBits * 0x11111111u;
+      if (row[t] >= 0) codes[static_cast<long long>(row[t]) * kLanes] = word;
     }
+    // Rows side by side have their scales side by side: a lane gathers those of one row, 32 bytes a warp.  (A byte a group and
+    // pass, as they come, took 18.0 us for 1600 rows of 2 x 16 heads, with the slower arithmetic of that time.)
+    const int from = lane / kStep * 8;                    // shift of the pass in which row i0 + lane was
+    uint32_t mine = 0;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+      mine |= ((__shfl_sync(0xffffffffu, bytes, (lane % kStep) * kLanes + g * 4) >> (from & 31)) & 255u) << (8 * g);
+    uint8_t *dst = (v ? p.v_scales : p.k_scales) + (w.row0 + srow) * kGroups;
+    if (srow >= 0) {
+      if constexpr (kGroups == 4) *reinterpret_cast<uint32_t *>(dst) = mine;
+      else *reinterpret_cast<uint16_t *>(dst) = static_cast<uint16_t>(mine);
+    }
+  }
 }
 
 template <int D>
-__global__ void __launch_bounds__(kKv4Threads) kv4_read_kernel(const __grid_constant__ Kv4Args p) {
+__device__ __forceinline__ void kv4_read_rows(const Kv4Args &p, const Kv4Place &w, int lane) {
   constexpr int kLanes = D / 8, kStep = 32 / kLanes;
-  pdl_wait();
-  pdl_launch_dependents();
-  Kv4Place w;
-  if (!kv4_place<D>(p, w)) return;
-  const int lane = threadIdx.x & 31, c = lane % kLanes, r0 = lane / kLanes;
+  const int c = lane % kLanes, r0 = lane / kLanes;
   bool bad = false;
   uint32_t word[2][kPasses], byte[2][kPasses];
   bool there[kPasses];
 #pragma unroll
   for (int t = 0; t < kPasses; ++t) {
-    const long long row = kv4_row(p, w, w.i0 + t * kStep + r0, bad);
-    there[t] = row >= 0;
+    const int pos = kv4_row(p, w, w.i0 + t * kStep + r0, bad);
+    there[t] = pos >= 0;
+    const long long row = w.row0 + pos;
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
       word[v][t] = there[t] ? __ldcs(reinterpret_cast<const uint32_t *>(v ? p.v_codes : p.k_codes) + row * kLanes + c) : 0u;
@@ -128,6 +141,7 @@ __global__ void __launch_bounds__(kKv4Threads) kv4_read_kernel(const __grid_cons
     }
   }
   if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, kStatusBadIndex);
+  const long long dst = w.b * p.out_elem + (w.i0 + r0) * p.out_row + w.h * p.out_head + c * 8;
 #pragma unroll
   for (int t = 0; t < kPasses; ++t)
 #pragma unroll
@@ -136,19 +150,32 @@ __global__ void __launch_bounds__(kKv4Threads) kv4_read_kernel(const __grid_cons
       const uint32_t s2 = kv4_scale2(byte[v][t]);
       uint32_t o[4];
       kv4_word(word[v][t], s2, kv4_offset2(s2), o);
-      bf16 *dst = (v ? p.v_out : p.k_out) + w.b * p.out_elem + (w.i0 + t * kStep + r0) * p.out_row + w.h * p.out_head + c * 8;
-      __stcs(reinterpret_cast<uint4 *>(dst), make_uint4(o[0], o[1], o[2], o[3]));
+      *reinterpret_cast<uint4 *>((v ? p.v_out : p.k_out) + dst + t * kStep * p.out_row) = make_uint4(o[0], o[1], o[2], o[3]);
     }
+}
+
+template <int D, bool WRITE>
+__global__ void __launch_bounds__(kKv4Threads) kv4_rows_kernel(const __grid_constant__ Kv4Args p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  for (int b = blockIdx.y; b < p.B; b += gridDim.y) {
+    Kv4Place w;
+    if (!kv4_place<D>(p, b, w)) continue;
+    if constexpr (WRITE) kv4_write_rows<D>(p, w, lane);
+    else kv4_read_rows<D>(p, w, lane);
+  }
 }
 
 cudaError_t launch_kv4_rows(bool write, Kv4Args a, cudaStream_t st) {
   const int rows = kPasses * (32 / (a.D / 8));
-  a.units = static_cast<long long>(a.B) * a.H * ((a.n + rows - 1) / rows);
-  const long long grid = (a.units + kKv4Threads / 32 - 1) / (kKv4Threads / 32);
-  if (grid > 0x7FFFFFFF) return cudaErrorInvalidValue;
-  const dim3 g(static_cast<unsigned>(grid)), b(kKv4Threads);
-  if (a.D == 64) return write ? launch_pdl(kv4_write_kernel<64>, g, b, 0, st, a) : launch_pdl(kv4_read_kernel<64>, g, b, 0, st, a);
-  return write ? launch_pdl(kv4_write_kernel<128>, g, b, 0, st, a) : launch_pdl(kv4_read_kernel<128>, g, b, 0, st, a);
+  const long long units = static_cast<long long>(a.H) * ((a.n + rows - 1) / rows);
+  if (units > 0x7FFFFFF0) return cudaErrorInvalidValue;
+  a.units = static_cast<int>(units);
+  a.div_h = make_fast_div(a.H, units);
+  const dim3 g(static_cast<unsigned>((units + kKv4Threads / 32 - 1) / (kKv4Threads / 32)), a.B < 65535 ? a.B : 65535), b(kKv4Threads);
+  if (a.D == 64) return write ? launch_pdl(kv4_rows_kernel<64, true>, g, b, 0, st, a) : launch_pdl(kv4_rows_kernel<64, false>, g, b, 0, st, a);
+  return write ? launch_pdl(kv4_rows_kernel<128, true>, g, b, 0, st, a) : launch_pdl(kv4_rows_kernel<128, false>, g, b, 0, st, a);
 }
 
 }  // namespace fvar
