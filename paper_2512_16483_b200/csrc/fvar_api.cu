@@ -77,6 +77,18 @@ bool tmap_kblocks(CUtensorMap *m, const void *base, uint64_t rows, uint64_t kblo
 }
 
 // Status word used by the kernel-level entry points (contexts carry their own in the workspace).
+bool tmap_codes(CUtensorMap *m, const void *codes, const Kv4AttnArgs &a, uint32_t rows) {
+  if (!tmap_init_driver()) return false;
+  const cuuint64_t row = a.D / 2;
+  cuuint64_t dims[4] = {row, static_cast<cuuint64_t>(a.L_cap), static_cast<cuuint64_t>(a.Hkv), static_cast<cuuint64_t>(a.B)};
+  cuuint64_t strides[3] = {row, row * a.L_cap, row * static_cast<cuuint64_t>(a.elem_stride)};
+  cuuint32_t box[4] = {static_cast<cuuint32_t>(row), rows, 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  a.D == 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 __device__ unsigned g_kernel_status;
 
 static std::string g_init_error;

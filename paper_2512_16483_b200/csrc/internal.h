@@ -322,6 +322,9 @@ struct Kv4AttnArgs {
   int kv_splits, tiles_per_cta, units;
   FastDiv div_nqt, div_h;
 };
+// Codes of keys or values: {D / 2 bytes, L_cap rows, heads, elements}, a box of `rows` rows of one head, swizzled over its own row
+// length (64 bytes: 16-byte column ^= row / 2 mod 4; 32 bytes: ^= row / 4 mod 2).
+bool tmap_codes(CUtensorMap *m, const void *codes, const Kv4AttnArgs &a, uint32_t rows);
 // More than 16 query rows a cache head: tcgen05 (attention_kv4_many.cu).
 cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st);
 // Bytes of workspace that such a call can use (0: none).

@@ -13,6 +13,11 @@ __device__ __forceinline__ uint32_t kv4_scale2(uint32_t byte) { return byte * 0x
 // The pair (s of lo, s of hi).
 __device__ __forceinline__ uint32_t kv4_scales(uint32_t lo, uint32_t hi) { return hi * 0x00100000u + (lo * 16u + (107u << 7) * 0x00010001u); }
 
+// The scale in byte g of four, as fp32.
+__device__ __forceinline__ float kv4_scale_f32(uint32_t bytes, int g) {
+  return __uint_as_float(__byte_perm(bytes, 0, 0x4440 + g) * 0x00100000u + (107u << 23));
+}
+
 __device__ __forceinline__ uint32_t fma_bf2(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d;
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));

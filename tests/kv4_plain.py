@@ -33,12 +33,17 @@ def unpack(codes):
 
 
 def attention(q, K, V, L, limits=None):
-    """q [B][r][H * D], K, V [B][Hkv][>= L][D] -> (result, sum of weight x |value|, largest sum of |q k| / sqrt(D)), the first two
-    [B][r][H * D], the last [B][r][H]: what the bounds of the kernels' rounding are made of."""
+    """q [B][r][H * D], K, V [B][Hkv][>= L][D] -> (result, sum of weight x |value|, bound of a score's error), the first two
+    [B][r][H * D], the last [B][r][H].
+
+    A score is a sum of D products in fp32 of queries with the numbers u of the cache, 0 to 15, less 8 times the sum of the
+    queries, times the groups' scales s: every term is at most 16 s |q|, and 16 s <= 16 / 7 of the group's greatest value (which is 7 s).
+    (D + 8) steps of 2^-23 of the sum of these, where a sum may be cut instead of rounded.  Where queries are split into two e4m3 terms
+    after scaling the row's greatest to at least 128, an element is off by half of e4m3's least step, 2^-10, at most: 2^-17 of the greatest."""
     B, r, _ = q.shape
     Hkv, D = K.shape[1], K.shape[3]
     H = q.shape[2] // D
-    out, mag, top = np.zeros((B, r, H, D)), np.zeros((B, r, H, D)), np.zeros((B, r, H))
+    out, mag, err = np.zeros((B, r, H, D)), np.zeros((B, r, H, D)), np.zeros((B, r, H))
     for b in range(B):
         n = np.full(r, L) if limits is None else np.clip(limits[b], 0, L)
         for h in range(H):
@@ -52,17 +57,18 @@ def attention(q, K, V, L, limits=None):
             w[some] /= w[some].sum(-1, keepdims=True)
             out[b, :, h], mag[b, :, h] = w @ v, w @ np.abs(v)
             if L:
-                top[b, :, h] = (np.abs(x) @ np.abs(k).T).max(-1) / np.sqrt(D)
-    return out.reshape(B, r, H * D), mag.reshape(B, r, H * D), top
+                steps = np.repeat(np.abs(k).reshape(L, -1, GROUP).max(-1), GROUP, -1) * (16.0 / 7.0)
+                err[b, :, h] = ((D + 8) * 2.0 ** -23 * (np.abs(x) @ steps.T).max(-1)
+                                + 2.0 ** -17 * np.abs(x).max(-1) * np.abs(k).sum(-1).max()) / np.sqrt(D)
+    return out.reshape(B, r, H * D), mag.reshape(B, r, H * D), err
 
 
-def bound(out, mag, top, L, D):
+def bound(out, mag, err, L, D):
     """How far a bf16 result of the kernels may be off.  With A = sum of weight x |value|: each weight is rounded to bf16 once
-    (2^-8 of A), the result once (2^-8 of it).  A score is a sum of D exact products in fp32, at most 2^-23 of the sum of their
-    magnitudes S off a step where a sum is cut instead of rounded, then one product with log2(e) / sqrt(D), one subtraction of
-    the maximum and an exp2 of 2^-22: every weight off by a factor within 1 +- 2 (D + 8) 2^-23 S + 2^-21, and the sum of the weights
-    too.  The weighted sum itself has at most L / 8 + 64 steps (keys come eight or more at a time, and ranges of keys are joined)."""
-    D_, r = mag.shape[-1] // top.shape[-1], mag.shape[1]
-    S = np.repeat(top, D_, -1)
-    rel = 2.0 ** -8 + 2 * (2 * (D + 8) * 2.0 ** -23 * S + 2.0 ** -21) + (L / 8 + 64) * 2.0 ** -23
+    (2^-8 of A), the result once (2^-8 of it).  A score is off by err, then comes one product with log2(e) / sqrt(D), one
+    subtraction of the maximum (2^-23 of the scores each, within twice err) and an exp2 of 2^-22: every weight off by a factor within
+    1 +- (2 err + 2^-21), and the sum of the weights too.  The weighted sum itself has at most L / 8 + 64 steps (keys come eight or more
+    at a time, and ranges of keys are joined)."""
+    e = np.repeat(err, mag.shape[-1] // err.shape[-1], -1)
+    rel = 2.0 ** -8 + 2 * (2 * e + 2.0 ** -21) + (L / 8 + 64) * 2.0 ** -23
     return rel * mag + 2.0 ** -8 * (np.abs(out) + rel * mag) + 1e-30

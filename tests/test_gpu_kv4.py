@@ -162,8 +162,8 @@ def _check(fv, q, kv, K, V, L, limits=None, q_dev=None, out=None):
     got = fv.fvar_attention_kv4(to_bf16_cuda(q) if q_dev is None else q_dev, kv, L,
                                 None if limits is None else torch.tensor(np.asarray(limits), dtype=torch.int32, device="cuda"), out=out)
     assert fv.kernel_poll_status() == fv.OK
-    ref, mag, top = kp.attention(q, K, V, L, limits)
-    over = np.abs(bf16_to_numpy(got) - ref) - kp.bound(ref, mag, top, L, K.shape[3])
+    ref, mag, err = kp.attention(q, K, V, L, limits)
+    over = np.abs(bf16_to_numpy(got) - ref) - kp.bound(ref, mag, err, L, K.shape[3])
     assert not np.isnan(over).any() and over.max() <= 0, (float(over.max()), np.unravel_index(over.argmax(), over.shape))
     return got
 
@@ -314,8 +314,8 @@ def test_scales_written_one_after_the_other_and_attended_to(fv):
     at = 0
     for x, got in zip(qkv, outs):
         at += x.shape[1]
-        ref, mag, top = kp.attention(x[..., :C], K, V, at)
-        assert np.all(np.abs(bf16_to_numpy(got) - ref) <= kp.bound(ref, mag, top, at, D))
+        ref, mag, err = kp.attention(x[..., :C], K, V, at)
+        assert np.all(np.abs(bf16_to_numpy(got) - ref) <= kp.bound(ref, mag, err, at, D))
     assert torch.equal(outs[-1], outs[-2][1::2])
 
     side = torch.cuda.Stream()
