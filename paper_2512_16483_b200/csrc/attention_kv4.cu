@@ -1,20 +1,14 @@
 // Attention of query rows over a cache in 4 bits (format and operator: include/fvar.h).
 //
-// Few rows (attention_kv4_few_kernel, 16 query rows a cache head at a time): bound by reading the cache, so the codes go from
-// memory to the tensor cores without a stop on the way: TMA brings them to shared memory as they are, a warp takes the codes of 16
-// keys into registers in the order in which mma.sync wants its operand, and decodes them there.  (Through tcgen05 they would have to
-// be decoded into shared memory and read from there again: 2.5 times their bf16 size at 128 bytes a clock, 1.8 times what
-// reading the codes from HBM takes.)  Keys and values are the operand of 16 rows, the query rows the one of 8:
+// Few rows (attention_kv4_few_kernel, up to 16 query rows a cache head): bound by reading the cache, so the codes go from
+// memory to the tensor cores without a stop on the way: bulk copies bring them to shared memory as they are, a warp takes the
+// codes of 16 keys into registers in the order in which mma.sync wants its operand and decodes them there.  (Through tcgen05 they would
+// have to be decoded into shared memory and read from there again: 2.5 times their bf16 size at 128 bytes a clock, 1.8 times
+// what reading the codes from HBM takes.)  Keys and values are the operand of 16 rows, the query rows the one of 8:
 //   S^T [16 keys][8 rows] = K Q^T,   O^T [16 of D][8 rows] += V^T P^T.
-// What bounds it is the arithmetic of decoding, so little of it is left:
-//   keys     A number u of 4 bits in a byte is u 2^-9 as e4m3, from 0 to 15 (below 8 a subnormal number, and the first binade above has
-//            the same step).  So one mask makes four operand elements of a word's even half-bytes, a shift and a mask those of the odd
-//            ones.  Queries are split into two e4m3 terms after scaling their row by a power of two to 128 .. 256: q = hi + lo, exact
-//            for elements above 2^-10 of the row's greatest, and off by 2^-18 of it at most below.  A product covers one group, and is
-//            scaled when it is added to the score: s += scale (acc - 8 sum q), the last term as the accumulator's first value.
-//   values   (128 + u) s - 136 s in bf16 pairs (kv4_pair), two keys in a register.
+// The order of D within a product is free, so a lane takes whole words: of a key row the words of its own quarter of D (that is
+// one group and one scale at D = 128), of four value rows one or two words each.
 #include <limits.h>
-#include <cuda_fp16.h>
 #include <math.h>
 
 #include "kv4.cuh"
@@ -27,24 +21,6 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// D[16][8] = A[16][32] B[32][8] + C, e4m3, fp32 accumulator.
-__device__ __forceinline__ void mma_16832(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1,
-                                          float c2, float c3) {
-  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
-               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
-}
-// Four floats as e4m3, the first in the lowest byte, and what they became.
-__device__ __forceinline__ uint32_t to_e4m3(const float (&x)[4], float (&back)[4]) {
-  uint16_t lo, hi;
-  uint32_t b0, b1;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[1]), "f"(x[0]));
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[3]), "f"(x[2]));
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(b0) : "h"(lo));
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(b1) : "h"(hi));
-  const float2 f0 = __half22float2(*reinterpret_cast<const __half2 *>(&b0)), f1 = __half22float2(*reinterpret_cast<const __half2 *>(&b1));
-  back[0] = f0.x; back[1] = f0.y; back[2] = f1.x; back[3] = f1.y;
-  return lo | static_cast<uint32_t>(hi) << 16;
-}
 // Transposes an 8 x 8 matrix of 16-bit elements that a warp holds two to a lane.
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
   uint32_t d;
@@ -54,16 +30,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
 __device__ __forceinline__ uint32_t pack_bf2(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ uint32_t ld_shared_u16(uint32_t addr) {
-  uint16_t v;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
-  return v;
-}
-__device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
-  return v;
 }
 __device__ __forceinline__ unsigned add_acq_rel(uint32_t addr, unsigned v) {
   unsigned old;
@@ -79,16 +45,16 @@ __device__ __forceinline__ void ld_shared_words(uint32_t addr, uint32_t (&w)[N])
 
 // Running maxima start here: finite, so that no difference of two of them is a NaN.
 constexpr float kNoMax = -3.0e38f;
-// What a query row's share of a range of keys weighs; maxima in units of log2.  A range without any key has l = 0.
-__device__ __forceinline__ float range_weight(float m, float l, float m_all) { return l == 0.f ? 0.f : exp2f(m - m_all); }
+// What a query row's share of a range of keys weighs; m in units of the scores, c of log2.  A range without any key has l = 0.
+__device__ __forceinline__ float range_weight(float m, float l, float m_all, float c) { return l == 0.f ? 0.f : exp2f((m - m_all) * c); }
 
+constexpr int kFewStages = 3;
 constexpr int kFewMaxRanges = 8;
 
 template <int D, int NB, int W>
 struct FewCfg {
-  static constexpr int kSets = NB == 1 ? 2 : 1;           // sets of 16 keys that a warp takes of a stage
-  static constexpr int kStages = NB == 1 ? 3 : 4;
-  static constexpr int kFewWarps = W, kFewThreads = 32 * W, kFewKeys = 16 * W, kFewStageKeys = kFewKeys * kSets;
+  static constexpr int kFewSets = NB == 1 || W == 8 ? 2 : 1;                  // sets of 16 keys that a warp takes of a stage
+  static constexpr int kFewWarps = W, kFewThreads = 32 * W, kFewKeys = 16 * W, kFewStageKeys = kFewKeys * kFewSets;
   static constexpr int kRows = 8 * NB;                    // query rows of a unit
   static constexpr int kCodeBytes = kFewStageKeys * D / 2, kScaleBytes = kFewStageKeys * D / kKv4Group;
   static constexpr int kStageBytes = 2 * (kCodeBytes + kScaleBytes);          // K codes, V codes, K scales, V scales
@@ -97,34 +63,25 @@ struct FewCfg {
   static constexpr int kQuads = kRows * D / 4;            // float4 of a unit
   static constexpr int kRecvBytes = (kQuads + kFewMaxRanges) * 16;            // what the ranges of a cluster push here
   static constexpr int kMlBytes = kFewMaxRanges * kRows * 8;
-  static constexpr int kTailBytes = 64;                   // barriers, counters, the abort flag
-  static constexpr int kQueryBytes = NB * (D / kKv4Group) * (32 * 16 + 8 * 4) + kRows * 4;   // e4m3 terms, first values, scales of the rows
-  static constexpr int kStagesBytes = kStages * kStageBytes, kAllParts = (kPartBytes + kFewWarps * kRows * 8 + 127) / 128 * 128;
+  static constexpr int kStagesBytes = kFewStages * kStageBytes, kAllParts = (kPartBytes + kFewWarps * kRows * 8 + 127) / 128 * 128;
   static constexpr int kFrontBytes = kStagesBytes > kAllParts ? kStagesBytes : kAllParts;
-  static constexpr int kSmemBytes = kFrontBytes + kRecvBytes + kMlBytes + kQueryBytes + kTailBytes;
-  static_assert(kCodeBytes % (4 * D) == 0 && kStageBytes % (4 * D) == 0, "the swizzle repeats after eight rows of codes");
+  static constexpr int kSmemBytes = kFrontBytes + kRecvBytes + kMlBytes + 128;
 };
 
 template <int D, int NB, int W>
-__global__ void __launch_bounds__(32 * W, 16 / W)
-attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Kv4AttnArgs p) {
+__global__ void __launch_bounds__(32 * W, NB == 1 ? 16 / W : 1) attention_kv4_few_kernel(const __grid_constant__ Kv4AttnArgs p) {
   using Cfg = FewCfg<D, NB, W>;
-  constexpr int kFewWarps = W, kFewThreads = 32 * W, kFewKeys = Cfg::kFewKeys, kFewStageKeys = Cfg::kFewStageKeys;
-  constexpr int kSets = Cfg::kSets, kFewStages = Cfg::kStages, NG = D / kKv4Group, VW = D / 64;      // groups of a row, words a lane takes of a value row
-  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  constexpr int kFewWarps = W, kFewThreads = 32 * W, kFewKeys = Cfg::kFewKeys, kFewStageKeys = Cfg::kFewStageKeys, kFewSets = Cfg::kFewSets;
+  constexpr int KW = D / 32, VW = D / 64;                 // words a lane takes of a key row, of a value row
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  __shared__ uint64_t bars[kFewStages];
+  __shared__ unsigned done[kFewStages];                   // warps that have finished with a slot, in all its uses
+  __shared__ volatile int abort_flag;
   const uint32_t stages = smem_u32(smem_raw);
   const uint32_t recv = stages + Cfg::kFrontBytes, recv_ml = recv + Cfg::kRecvBytes;
-  const uint32_t q_terms = recv_ml + Cfg::kMlBytes, q_first = q_terms + NB * NG * 512, q_scale = q_first + NB * NG * 32;
-  uint8_t *tail = smem_raw + Cfg::kSmemBytes - Cfg::kTailBytes;
-  auto full = [&](int s) { return smem_u32(tail) + 8 * s; };
-  unsigned *done = reinterpret_cast<unsigned *>(tail + 8 * kFewStages);        // warps that have finished with a slot, in all its uses
-  volatile int &abort_flag = *reinterpret_cast<volatile int *>(tail + 12 * kFewStages);
+  auto full = [&](int s) { return smem_u32(&bars[s]); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
   const long long wb = wait_budget(p.wait_cycles);
-  if (stages & 1023) {                                    // the swizzle counts from 1024-byte boundaries
-    if (threadIdx.x == 0) atomicOr(p.status, kStatusTimeout);
-    return;
-  }
 
   if (threadIdx.x == 0) {
     abort_flag = 0;
@@ -161,6 +118,7 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
   const int nst = (k1 - k0 + kFewStageKeys - 1) / kFewStageKeys;
   const long long row0 = b * p.elem_stride + static_cast<long long>(kv) * p.L_cap;
 
+  const float c = p.scale_log2;
   float o[NB][D / 16][4];
   float m[NB][2], l[NB][2];
 #pragma unroll
@@ -177,169 +135,102 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
   auto request = [&](int st) {
     const int slot = st % kFewStages, k = k0 + st * kFewStageKeys;
     const uint32_t n = min(kFewStageKeys, kend - k), dst = stages + slot * Cfg::kStageBytes;
-    mbar_expect_tx(full(slot), 2 * Cfg::kCodeBytes + n * 2 * NG);
-    tma_load_4d(dst, &tmK, full(slot), 0, k, kv, b);       // rows beyond L_cap become zeros, others nobody sees are masked
-    bulk_load(dst + 2 * Cfg::kCodeBytes, p.k_scales + (row0 + k) * NG, n * NG, full(slot));
-    tma_load_4d(dst + Cfg::kCodeBytes, &tmV, full(slot), 0, k, kv, b);
-    bulk_load(dst + 2 * Cfg::kCodeBytes + Cfg::kScaleBytes, p.v_scales + (row0 + k) * NG, n * NG, full(slot));
+    mbar_expect_tx(full(slot), n * (D + 2 * (D / kKv4Group)));
+    bulk_load(dst, p.k_codes + (row0 + k) * (D / 2), n * (D / 2), full(slot));
+    bulk_load(dst + 2 * Cfg::kCodeBytes, p.k_scales + (row0 + k) * (D / kKv4Group), n * (D / kKv4Group), full(slot));
+    bulk_load(dst + Cfg::kCodeBytes, p.v_codes + (row0 + k) * (D / 2), n * (D / 2), full(slot));
+    bulk_load(dst + 2 * Cfg::kCodeBytes + Cfg::kScaleBytes, p.v_scales + (row0 + k) * (D / kKv4Group), n * (D / kKv4Group), full(slot));
   };
   if (threadIdx.x == 0)
     for (int st = 0; st < min(kFewStages, nst); ++st) request(st);
-  // ------------------------------------------------------------------ queries
-  // Warp nb prepares rows 8 nb ..: a lane's 8 values of each group become 4 + 4 bytes of the product's second operand, in the order
-  // in which the masks leave the codes of a word (values 0, 4, 1, 5 and 2, 6, 3, 7).
-  for (int nb = warp; nb < NB; nb += W) {
-    const int rho = rho0 + nb * 8 + gid;
-    const bool there = rho < nrows;
-    const bf16 *src = p.q + (there ? (static_cast<long long>(b) * p.r + rho / G) * p.ldq + (kv * G + rho % G) * D + tig * 8 : 0);
-    uint4 raw[NG];
-    uint32_t top2 = 0;                                    // maxima of the bit patterns: ordered as the magnitudes are
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      raw[g] = there ? *reinterpret_cast<const uint4 *>(src + g * kKv4Group) : make_uint4(0, 0, 0, 0);
-      top2 = __vmaxu2(top2, __vmaxu2(__vmaxu2(raw[g].x & 0x7FFF7FFFu, raw[g].y & 0x7FFF7FFFu), __vmaxu2(raw[g].z & 0x7FFF7FFFu, raw[g].w & 0x7FFF7FFFu)));
-    }
-    top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 1));
-    top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 2));
-    const int e = static_cast<int>(max(top2 & 0xFFFFu, top2 >> 16) >> 7);                    // biased exponent of the greatest; 255: infinite or NaN
-    // q * 2^(134 - e) in two steps, as the factor may be beyond fp32; rows of denormal numbers only come out smaller than 128
-    const int sh = 134 - max(e, 1);
-    const float f1 = __uint_as_float(static_cast<uint32_t>(127 + (sh >> 1)) << 23), f2 = __uint_as_float(static_cast<uint32_t>(127 + sh - (sh >> 1)) << 23);
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const uint32_t w[4] = {raw[g].x, raw[g].y, raw[g].z, raw[g].w};
-      float x[8], sum = 0.f;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[2 * k] = __uint_as_float(w[k] << 16) * f1 * f2;
-        x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u) * f1 * f2;
-      }
-      uint32_t term[4];
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {              // values 0, 4, 1, 5, then 2, 6, 3, 7
-        const float y[4] = {x[2 * half], x[2 * half + 4], x[2 * half + 1], x[2 * half + 5]};
-        float hi[4], rest[4], lo[4];
-        term[half] = to_e4m3(y, hi);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) rest[k] = y[k] - hi[k];
-        term[2 + half] = to_e4m3(rest, lo);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sum += hi[k] + lo[k];
-      }
-      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_terms + ((nb * NG + g) * 32 + lane) * 16), "r"(term[0]), "r"(term[1]), "r"(term[2]), "r"(term[3]) : "memory");
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      if (tig == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(q_first + ((nb * NG + g) * 8 + gid) * 4), "f"(sum * (-8.f / 512.f)) : "memory");
-    }
-    // scores in units of log2: 2^9 for the codes, 2^-sh for the queries; a row with an infinity or a NaN is NaN
-    const float f = e == 255 ? __uint_as_float(0x7FC00000u) : p.scale_log2 * 512.f / f1 / f2;
-    if (tig == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(q_scale + (nb * 8 + gid) * 4), "f"(f) : "memory");
-  }
-  __syncthreads();
   {
     // ------------------------------------------------------------------ products
-    uint32_t qt[NB][NG][4];
-    float2 first[NB][NG], c[NB];                          // of rows 2 tig and 2 tig + 1
+    uint32_t q[NB][KW][4];                                // [word][pair]: the lane's values of row rho0 + 8 nb + gid
     int lim[NB][2];
-    auto load_terms = [&](int nb, int g) { ld_shared_words<4>(q_terms + ((nb * NG + g) * 32 + lane) * 16, qt[nb][g]); };
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
+      const int rho = rho0 + nb * 8 + gid;
+      const bool there = rho < nrows;
+      const bf16 *src = p.q + (static_cast<long long>(b) * p.r + rho / G) * p.ldq + (kv * G + rho % G) * D + tig * (D / 4);
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        if (NB == 1) load_terms(nb, g);
-        if (NB == 1) first[nb][g] = ld_shared_f2(q_first + ((nb * NG + g) * 8 + 2 * tig) * 4);
+      for (int w = 0; w < KW; ++w) {
+        const uint4 v = there ? *reinterpret_cast<const uint4 *>(src + 8 * w) : make_uint4(0, 0, 0, 0);
+        q[nb][w][0] = v.x; q[nb][w][1] = v.y; q[nb][w][2] = v.z; q[nb][w][3] = v.w;
       }
-      c[nb] = ld_shared_f2(q_scale + (nb * 8 + 2 * tig) * 4);
 #pragma unroll
       for (int i = 0; i < 2; ++i) lim[nb][i] = min(limit_of(rho0 + nb * 8 + 2 * tig + i), k1);
     }
-    // Which key of a set is row gid of the first operand, and which are the four whose values a lane takes (as k 2 tig, 2 tig + 1,
-    // 2 tig + 8, 2 tig + 9 of the second product): free to choose as long as both agree, and such that the lanes of a load fall into
-    // different banks of the swizzled tile.
-    const int krow = D == 128 ? ((gid >> 1) & 1) + 4 * (gid >> 2) + 2 * (gid & 1) : (gid >> 1) + 4 * (gid & 1);
-    auto vrow = [&](int i) { return (D == 128 ? (tig & 1) + 4 * (tig >> 1) + 2 * (i & 1) : tig + 4 * (i & 1)) + 8 * (i >> 1); };
-    // 16-byte column of a row of codes in the swizzled tile
-    auto column = [&](int row, int ch) { return D == 128 ? ch ^ ((row >> 1) & 3) : ch ^ ((row >> 2) & 1); };
+    const float grow = 8.f / c;
     bool ok = true;
     for (int st = 0; st < nst; ++st) {
       const int slot = st % kFewStages;
       ok = __all_sync(0xffffffffu, mbar_wait(full(slot), (st / kFewStages) & 1, p.status, &abort_flag, wb));
       if (!ok) break;
-      const uint32_t base = stages + slot * Cfg::kStageBytes, kbase = base, vbase = base + Cfg::kCodeBytes;
-      const uint32_t ksbase = base + 2 * Cfg::kCodeBytes, vsbase = ksbase + Cfg::kScaleBytes;
-      const int kr = warp * 16 * kSets, key = k0 + st * kFewStageKeys + kr;                  // the warp's keys
+      const uint32_t base = stages + slot * Cfg::kStageBytes;
+      const int kr = warp * 16 * kFewSets, key = k0 + st * kFewStageKeys + kr;               // the warp's keys
       if (key < k1) {
-        uint32_t kw[kSets][2][NG], ks[kSets][2], vw[kSets][4][VW], vs[kSets][4];
+        uint32_t kw[kFewSets][2][KW], vw[kFewSets][4][VW], ks[kFewSets][2], vs[kFewSets][4];
 #pragma unroll
-        for (int x = 0; x < kSets; ++x)
+        for (int x = 0; x < kFewSets; ++x) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const int row = kr + 16 * x + krow + 8 * i;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-              uint32_t one[1];
-              ld_shared_words<1>(kbase + row * (D / 2) + column(row, g) * 16 + tig * 4, one);
-              kw[x][i][g] = one[0];
-            }
-            if constexpr (NG == 4) {
-              uint32_t one[1];
-              ld_shared_words<1>(ksbase + row * NG, one);
-              ks[x][i] = one[0];
-            } else {
-              ks[x][i] = ld_shared_u16(ksbase + row * NG);
-            }
+            const int row = kr + 16 * x + gid + 8 * i;
+            ld_shared_words<KW>(base + row * (D / 2) + tig * (D / 8), kw[x][i]);
+            ks[x][i] = ld_shared_u8(base + 2 * Cfg::kCodeBytes + row * (D / kKv4Group) + tig * (D / 4) / kKv4Group);
           }
+        }
+        // S^T = K Q^T: lane (gid, tig) has quarter tig of keys gid and gid + 8 of a set
+        float s[kFewSets][NB][4], s_odd[kFewSets][NB][4];
 #pragma unroll
-        for (int x = 0; x < kSets; ++x)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int row = kr + 16 * x + vrow(i);
-            ld_shared_words<VW>(vbase + row * (D / 2) + column(row, gid * (D / 16) / 16) * 16 + gid * (D / 16) % 16, vw[x][i]);
-            vs[x][i] = ld_shared_u8(vsbase + row * NG + gid * (D / 8) / kKv4Group);
-          }
-        // S^T: lane (gid, tig) has scores of keys krow and krow + 8 and of rows 2 tig and 2 tig + 1
-        float s[kSets][NB][4];
-#pragma unroll
-        for (int x = 0; x < kSets; ++x)
+        for (int x = 0; x < kFewSets; ++x)
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[x][nb][k] = 0.f;
+            for (int k = 0; k < 4; ++k) s[x][nb][k] = s_odd[x][nb][k] = 0.f;
+        uint32_t s0[kFewSets], s1[kFewSets], f0[kFewSets], f1[kFewSets];
 #pragma unroll
-        for (int g = 0; g < NG; ++g)
+        for (int x = 0; x < kFewSets; ++x) {
+          s0[x] = kv4_scale2(ks[x][0]);
+          s1[x] = kv4_scale2(ks[x][1]);
+          f0[x] = kv4_offset2(s0[x]);
+          f1[x] = kv4_offset2(s1[x]);
+        }
 #pragma unroll
-          for (int x = 0; x < kSets; ++x) {
-            const uint32_t a0 = kw[x][0][g] & 0x0F0F0F0Fu, a1 = kw[x][1][g] & 0x0F0F0F0Fu;
-            const uint32_t a2 = kw[x][0][g] >> 4 & 0x0F0F0F0Fu, a3 = kw[x][1][g] >> 4 & 0x0F0F0F0Fu;
-            const float sc0 = kv4_scale_f32(ks[x][0], g), sc1 = kv4_scale_f32(ks[x][1], g);
+        for (int w = 0; w < KW; ++w)
+#pragma unroll
+          for (int x = 0; x < kFewSets; ++x) {
+            uint32_t a[4], a8[4];
+            kv4_word(kw[x][0][w], s0[x], f0[x], a);
+            kv4_word(kw[x][1][w], s1[x], f1[x], a8);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-              if (NB > 1) load_terms(nb, g);
-              const float2 f = NB == 1 ? first[nb][g] : ld_shared_f2(q_first + ((nb * NG + g) * 8 + 2 * tig) * 4);
-              float acc[4];
-              mma_16832(acc, a0, a1, a2, a3, qt[nb][g][0], qt[nb][g][1], f.x, f.y, f.x, f.y);
-              mma_16832(acc, a0, a1, a2, a3, qt[nb][g][2], qt[nb][g][3], acc[0], acc[1], acc[2], acc[3]);
-              s[x][nb][0] = fmaf(acc[0], sc0, s[x][nb][0]);
-              s[x][nb][1] = fmaf(acc[1], sc0, s[x][nb][1]);
-              s[x][nb][2] = fmaf(acc[2], sc1, s[x][nb][2]);
-              s[x][nb][3] = fmaf(acc[3], sc1, s[x][nb][3]);
+              mma_16816(s[x][nb], a[0], a8[0], a[1], a8[1], q[nb][w][0], q[nb][w][1]);
+              mma_16816(s_odd[x][nb], a[2], a8[2], a[3], a8[3], q[nb][w][2], q[nb][w][3]);
             }
           }
-        // in units of log2
 #pragma unroll
-        for (int x = 0; x < kSets; ++x)
+        for (int x = 0; x < kFewSets; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {                   // keys 2 tig, 2 tig + 1, 2 tig + 8, 2 tig + 9; values gid * D / 8 ...
+            const int row = kr + 16 * x + 2 * tig + (i & 1) + 8 * (i >> 1);
+            ld_shared_words<VW>(base + Cfg::kCodeBytes + row * (D / 2) + gid * (D / 16), vw[x][i]);
+            vs[x][i] = ld_shared_u8(base + 2 * Cfg::kCodeBytes + Cfg::kScaleBytes + row * (D / kKv4Group) + gid * (D / 8) / kKv4Group);
+          }
+#pragma unroll
+        for (int x = 0; x < kFewSets; ++x)
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[x][nb][k] *= k & 1 ? c[nb].y : c[nb].x;
-        if (key + 16 * kSets > kmin) {
+            for (int k = 0; k < 4; ++k) s[x][nb][k] += s_odd[x][nb][k];          // two chains of products: 1.3 % of a launch
+        // s[x][nb][0 .. 3]: (key gid, row 2 tig), (gid, 2 tig + 1), (gid + 8, 2 tig), (gid + 8, 2 tig + 1)
+        if (key + 16 * kFewSets > kmin) {
 #pragma unroll
-          for (int x = 0; x < kSets; ++x)
+          for (int x = 0; x < kFewSets; ++x)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if (key + 16 * x + krow + 8 * (k >> 1) >= lim[nb][k & 1]) s[x][nb][k] = -INFINITY;
+                if (key + 16 * x + gid + 8 * (k >> 1) >= lim[nb][k & 1]) s[x][nb][k] = -INFINITY;
         }
         bool need = false;
         float top[NB][2];
@@ -349,8 +240,8 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
           for (int i = 0; i < 2; ++i) {
             top[nb][i] = fmaxf(s[0][nb][i], s[0][nb][i + 2]);
 #pragma unroll
-            for (int x = 1; x < kSets; ++x) top[nb][i] = fmaxf(top[nb][i], fmaxf(s[x][nb][i], s[x][nb][i + 2]));
-            need = need || top[nb][i] > m[nb][i] + 8.f;
+            for (int x = 1; x < kFewSets; ++x) top[nb][i] = fmaxf(top[nb][i], fmaxf(s[x][nb][i], s[x][nb][i + 2]));
+            need = need || top[nb][i] > m[nb][i] + grow;
           }
         // the accumulators are scaled anew only when a maximum has grown by more than 2^8 (and at the first keys)
         if (__any_sync(0xffffffffu, need)) {
@@ -361,7 +252,7 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
               float t2 = top[nb][i];
 #pragma unroll
               for (int d = 4; d < 32; d <<= 1) t2 = fmaxf(t2, __shfl_xor_sync(0xffffffffu, t2, d));
-              const float m2 = fmaxf(m[nb][i], t2), a = exp2f(m[nb][i] - m2);
+              const float m2 = fmaxf(m[nb][i], t2), a = exp2f((m[nb][i] - m2) * c);
               m[nb][i] = m2;
               l[nb][i] *= a;
 #pragma unroll
@@ -372,13 +263,13 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
             }
         }
 #pragma unroll
-        for (int x = 0; x < kSets; ++x) {
-          uint32_t pt[NB][2];                             // P^T of the set's two halves, as the second operand wants it
+        for (int x = 0; x < kFewSets; ++x) {
+          uint32_t pt[NB][2];                             // P^T of keys 0 - 7 and 8 - 15, as the second operand wants it
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
             float e[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) e[k] = exp2f(s[x][nb][k] - m[nb][k & 1]);
+            for (int k = 0; k < 4; ++k) e[k] = exp2f(fmaf(s[x][nb][k], c, -m[nb][k & 1] * c));
             l[nb][0] += e[0] + e[2];
             l[nb][1] += e[1] + e[3];
             pt[nb][0] = transpose_8x8(pack_bf2(e[0], e[1]));
@@ -447,7 +338,7 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < kFewWarps; ++w) {
-      const float a = range_weight(ml[w].x, ml[w].y, m_all);
+      const float a = range_weight(ml[w].x, ml[w].y, m_all, c);
       const float4 v = ld_shared_f4(part + (w * Cfg::kRows + row) * Cfg::kPitch + d * 4);
       acc.x = fmaf(a, v.x, acc.x); acc.y = fmaf(a, v.y, acc.y); acc.z = fmaf(a, v.z, acc.z); acc.w = fmaf(a, v.w, acc.w);
       l_all = fmaf(a, ml[w].y, l_all);
@@ -478,7 +369,7 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int t = 0; t < splits; ++t) {
         const float2 ml = ld_shared_f2(recv_ml + (t * Cfg::kRows + row) * 8);
-        const float a = range_weight(ml.x, ml.y, m_all);
+        const float a = range_weight(ml.x, ml.y, m_all, c);
         const float4 v = ld_shared_f4(recv + (t * cnt + y) * 16);
         acc.x = fmaf(a, v.x, acc.x); acc.y = fmaf(a, v.y, acc.y); acc.z = fmaf(a, v.z, acc.z); acc.w = fmaf(a, v.w, acc.w);
         l_all = fmaf(a, ml.y, l_all);
@@ -491,10 +382,11 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
   }
 }
 
-int g_few_force = 0;
+int g_few_force = 0, g_few_w = 8;
 template <int D, int NB, int W>
 static cudaError_t launch_few(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
   using Cfg = FewCfg<D, NB, W>;
+  constexpr int kFewThreads = 32 * W, kFewKeys = Cfg::kFewKeys;
   static unsigned long long prepared = 0;                 // a bit a device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -504,19 +396,17 @@ static cudaError_t launch_few(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     if (dev < 64) prepared |= 1ull << dev;
   }
-  CUtensorMap tk, tv;
-  if (!tmap_codes(&tk, a.k_codes, a, Cfg::kFewStageKeys) || !tmap_codes(&tv, a.v_codes, a, Cfg::kFewStageKeys)) return cudaErrorInvalidValue;
   const int tiles = (a.r * (a.H / a.Hkv) + Cfg::kRows - 1) / Cfg::kRows;
   const long long units = static_cast<long long>(tiles) * a.Hkv * a.B;
   if (a.Hkv > 65535 || a.B > 65535) return cudaErrorInvalidConfiguration;
-  const int rounds = (a.L + Cfg::kFewKeys - 1) / Cfg::kFewKeys;
+  const int rounds = (a.L + kFewKeys - 1) / kFewKeys;
   int s = 1;
   while (s < kFewMaxRanges && units * s < 2 * num_sms && rounds >= 2 * (s * 2)) s *= 2;
   if (g_few_force) s = g_few_force;
   a.kv_splits = s;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(tiles * s, a.Hkv, a.B);
-  cfg.blockDim = dim3(Cfg::kFewThreads);
+  cfg.blockDim = dim3(kFewThreads);
   cfg.dynamicSmemBytes = Cfg::kSmemBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -530,15 +420,15 @@ static cudaError_t launch_few(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
   if (one_predecessor(st)) attr[n++] = pdl_attribute();
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, attention_kv4_few_kernel<D, NB, W>, tk, tv, a);
+  return cudaLaunchKernelEx(&cfg, attention_kv4_few_kernel<D, NB, W>, a);
 }
 
 int g_few_rows = 16;
 cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {
   if (a.r * static_cast<long long>(a.H / a.Hkv) > g_few_rows) return launch_attention_kv4_many(a, workspace, bytes, num_sms, st);
   const bool one = a.r * static_cast<long long>(a.H / a.Hkv) <= 8;
-  if (a.D == 64) return one ? launch_few<64, 1, 8>(a, num_sms, st) : launch_few<64, 2, 8>(a, num_sms, st);
-  return one ? launch_few<128, 1, 8>(a, num_sms, st) : launch_few<128, 2, 8>(a, num_sms, st);
+  if (a.D == 64) return one ? launch_few<64, 1, 8>(a, num_sms, st) : g_few_w == 12 ? launch_few<64, 2, 12>(a, num_sms, st) : launch_few<64, 2, 8>(a, num_sms, st);
+  return one ? launch_few<128, 1, 8>(a, num_sms, st) : g_few_w == 12 ? launch_few<128, 2, 12>(a, num_sms, st) : launch_few<128, 2, 8>(a, num_sms, st);
 }
 
 }  // namespace fvar

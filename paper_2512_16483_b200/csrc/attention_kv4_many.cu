@@ -3,8 +3,9 @@
 // A unit of work is up to 256 query rows (two tiles of 128) of one cache head of one element; with grouped heads the rows of all
 // heads of the group, rho = row * G + head of the group.  One CTA of 16 warps:
 //   warp 0             issues S_t = Q_t K^T and O_t += P_t V, accumulators in TMEM;
-//   warps 1-7          decode: the codes of 128 keys or their values come from memory into registers a block ahead, and leave as the
-//                      bf16 operand tile, swizzled, in a ring of shared-memory slots; they bring the queries too;
+//   warp 7             requests the queries and, tile by tile, the codes and scales of 128 keys or their values (TMA);
+//   warps 1-6          decode, two warps a tile: codes from shared memory to registers, and back as the bf16 operand tile, swizzled, in
+//                      a ring of slots of its own;
 //   warps 8-11, 12-15  softmax of stream 0 and 1, one query row a thread.
 // The two streams are the two query tiles, out of phase, or with a lone tile the even and the odd blocks of keys.  A decoded
 // tile serves both query tiles.  Keys and values have the same layout, rows of D: the keys are a K-major operand, the values an
@@ -25,54 +26,56 @@
 
 namespace fvar {
 
-// bytes a multiple of 16, src 16-byte aligned.
-__device__ __forceinline__ void l2_fetch(const void *src, uint32_t bytes) {
-  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
-}
-
 constexpr int kManyThreads = 512;
-constexpr int kDecodeWarps = 7, kManySoftmaxWarp = 8;
+constexpr int kDecodeTeams = 3, kQueryWarp = 7, kManySoftmaxWarp = 8;      // teams of two warps
 // Registers a thread after the split: 2 * 72 + 2 * 184 = 4 * 128.
 constexpr int kRegsLaunch = 128, kRegsDecode = 72, kRegsRows = 184;
 static_assert(2 * kRegsDecode + 2 * kRegsRows == 4 * kRegsLaunch, "what is given back is what is taken");
-constexpr int kFetchAhead = 4;                // blocks
 constexpr int kTileRows = 128, kBlockKeys = 128;
 constexpr int kAtom = 128 * 128;              // [128 rows][64 bf16], swizzled
 constexpr float kGrow = 8.0f;                 // log2 units
 constexpr float kNoRowMax = -3.0e38f;         // running maxima start here: finite, so that no difference of two of them is a NaN
 constexpr int kManyMaxRanges = 6;
 
-template <int D>
+template <int D, bool CODES>
 struct ManyCfg {
   static constexpr int kTileBytes = 128 * D * 2;          // a query tile, a tile of 128 keys or of their values
-  static constexpr int kRing = D == 64 ? 10 : 5;
+  static constexpr int kRing = CODES ? (D == 64 ? 8 : 3) : (D == 64 ? 10 : 5);
+  static constexpr int kCodeBytes = kBlockKeys * D / 2, kScaleBytes = kBlockKeys * D / kKv4Group;
+  static constexpr int kRawBytes = kCodeBytes + kScaleBytes, kRaw = CODES ? (D == 64 ? 14 : 7) : 0;         // tiles of codes under way
   static constexpr int kQBytes = 2 * kTileBytes, kSwapBytes = 2 * kTileRows * 8;
-  static constexpr int kBars = 12 + 2 * kRing;
-  static constexpr int kSmemBytes = kQBytes + kRing * kTileBytes + kSwapBytes + 320;
+  static constexpr int kBars = 16 + 2 * kRing + 2 * kRaw;
+  static constexpr int kSmemBytes = kQBytes + kRing * kTileBytes + kRaw * kRawBytes + kSwapBytes + 512;
   static constexpr int kTmemCols = 512;                   // S0, S1, O0, O1
-  static_assert(kBars * 8 + 16 <= 320 && kSmemBytes <= 232448, "shared memory");
+  static_assert(kBars * 8 + 16 <= 512 && kSmemBytes <= 232448, "shared memory");
   static_assert(kSmemBytes > 116 * 1024, "one CTA per SM (the CTA allocates all of TMEM)");
+  static_assert(kRawBytes % (4 * D) == 0, "the swizzle of codes repeats after eight rows");
 };
 
 template <int D, bool RANGES, bool CODES>
 __global__ void __launch_bounds__(kManyThreads, 1)
-attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Kv4AttnArgs p) {
-  using Cfg = ManyCfg<D>;
-  constexpr int NR = Cfg::kRing;
+attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Kv4AttnArgs p) {
+  using Cfg = ManyCfg<D, CODES>;
+  constexpr int NR = Cfg::kRing, NC = Cfg::kRaw;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  const uint32_t q_smem = smem_u32(smem_raw), ring_smem = q_smem + Cfg::kQBytes, swap_smem = ring_smem + NR * Cfg::kTileBytes;
+  const uint32_t q_smem = smem_u32(smem_raw), ring_smem = q_smem + Cfg::kQBytes, raw_smem = ring_smem + NR * Cfg::kTileBytes;
+  const uint32_t swap_smem = raw_smem + NC * Cfg::kRawBytes;
   const uint32_t bar_base = swap_smem + Cfg::kSwapBytes;
-  uint8_t *tail = smem_raw + Cfg::kQBytes + NR * Cfg::kTileBytes + Cfg::kSwapBytes + 8 * Cfg::kBars;
+  uint8_t *tail = smem_raw + Cfg::kSmemBytes - 512 + 8 * Cfg::kBars;
   uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(tail);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 4);
-  const uint32_t q_full = bar_base, q_empty = bar_base + 8;
-  auto ring_full = [&](int s) { return bar_base + 8u * (2 + s); };
-  auto ring_empty = [&](int s) { return bar_base + 8u * (2 + NR + s); };
-  auto s_full = [&](int t) { return bar_base + 8u * (2 + 2 * NR + t); };
-  auto p_half = [&](int t) { return bar_base + 8u * (4 + 2 * NR + t); };
-  auto p_full = [&](int t) { return bar_base + 8u * (6 + 2 * NR + t); };
-  auto o_full = [&](int t) { return bar_base + 8u * (8 + 2 * NR + t); };   // P V of a block that is not the stream's last
-  auto o_last = [&](int t) { return bar_base + 8u * (10 + 2 * NR + t); };
+  auto q_full = [&](int s) { return bar_base + 8u * s; };
+  auto q_empty = [&](int s) { return bar_base + 8u * (2 + s); };
+  auto ring_full = [&](int s) { return bar_base + 8u * (4 + s); };
+  auto ring_empty = [&](int s) { return bar_base + 8u * (4 + NR + s); };
+  auto s_full = [&](int t) { return bar_base + 8u * (4 + 2 * NR + t); };
+  auto p_half = [&](int t) { return bar_base + 8u * (6 + 2 * NR + t); };
+  auto p_full = [&](int t) { return bar_base + 8u * (8 + 2 * NR + t); };
+  auto o_full = [&](int t) { return bar_base + 8u * (10 + 2 * NR + t); };   // P V of a block that is not the stream's last
+  auto o_last = [&](int t) { return bar_base + 8u * (12 + 2 * NR + t); };
+  const uint32_t swap_full = bar_base + 8u * (14 + 2 * NR), swap_done = swap_full + 8;       // a lone tile's streams meet; both have stored their columns
+  auto raw_full = [&](int s) { return bar_base + 8u * (16 + 2 * NR + s); };
+  auto raw_empty = [&](int s) { return bar_base + 8u * (16 + 2 * NR + NC + s); };
 
   if (q_smem & 1023) {                                    // the swizzle counts from 1024-byte boundaries
     if (threadIdx.x == 0) atomicOr(p.status, kStatusTimeout);
@@ -82,11 +85,17 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
   const long long wb = wait_budget(p.wait_cycles);
   if (threadIdx.x == 0) {
     *abort_flag = 0;
-    mbar_init(q_full, kDecodeWarps);
-    mbar_init(q_empty, 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(q_full(s), 1);
+      mbar_init(q_empty(s), 1);
+    }
     for (int s = 0; s < NR; ++s) {
-      mbar_init(ring_full(s), CODES ? kDecodeWarps : 1);
+      mbar_init(ring_full(s), CODES ? 2 : 1);
       mbar_init(ring_empty(s), 1);
+    }
+    for (int s = 0; s < NC; ++s) {
+      mbar_init(raw_full(s), 1);
+      mbar_init(raw_empty(s), 2);
     }
     for (int t = 0; t < 2; ++t) {
       mbar_init(s_full(t), 1);
@@ -95,6 +104,8 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
       mbar_init(o_full(t), 1);
       mbar_init(o_last(t), 1);
     }
+    mbar_init(swap_full, 256);
+    mbar_init(swap_done, 256);
     mbar_fence_init();
   }
   if (warp == 0) {
@@ -111,6 +122,8 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
   // Units: RANGES: the CTAs of a cluster take the key ranges of one; else a CTA walks the units blockIdx.x, + gridDim.x, ...
   const int splits = RANGES ? p.kv_splits : 1, sp = RANGES ? static_cast<int>(blockIdx.x) % splits : 0;
   const int unit0 = RANGES ? static_cast<int>(blockIdx.x) / splits : blockIdx.x, unit_step = RANGES ? p.units : gridDim.x;
+  // Lone tiles have room for the queries of two units, pairs fill it with one's.
+  const uint32_t qrooms = p.tiles_per_cta == 1 ? 2 : 1;
   const int G = p.H / p.Hkv, nrows = p.r * G;
   struct Unit {
     int rho0, h, e, ntiles, kb0, nkv, keys;               // keys: those that some row of the unit sees; blocks [kb0, kb0 + nkv) here
@@ -124,7 +137,7 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
     x.ntiles = (p.tiles_per_cta == 2 && nrows - x.rho0 > kTileRows) ? 2 : 1;
     x.keys = p.L;
     if (p.limits) {
-      const int i0 = x.rho0 / G, i1 = (min(nrows, x.rho0 + x.ntiles * kTileRows) - 1) / G;
+      const int i0 = fast_div(x.rho0, p.div_g), i1 = fast_div(min(nrows, x.rho0 + x.ntiles * kTileRows) - 1, p.div_g);
       int top = 0;
       for (int i = i0 + lane; i <= i1; i += 32) top = max(top, p.limits[static_cast<long long>(x.e) * p.r + i]);
       x.keys = min(__reduce_max_sync(0xffffffffu, top), p.L);
@@ -170,7 +183,7 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
       for (int k = 0; k < 4; ++k) umma_bf16_tmem_a_if(leader, to, tp + 8 * k, dv + k * (16 * 128 >> 4), idesc_o, (accumulate || k != 0) ? 1u : 0u);
     };
     bool ok = true;
-    uint32_t q_par = 0, p_par = 0, phase = 0;           // p_par: a bit a stream
+    uint32_t qn = 0, p_par = 0, phase = 0;           // p_par: a bit a stream
     int slot = 0;
     auto take = [&]() {                                 // the next tile of the ring; its slot
       const int s = slot;
@@ -197,15 +210,16 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
       const Unit x = unit_at(u);
       const int nkv = x.nkv;
       if (nkv == 0) continue;
-      ok = wait(q_full, q_par);
-      q_par ^= 1u;
+      const int room = qn % qrooms;
+      ok = wait(q_full(room), qn / qrooms & 1u);
+      ++qn;
       if (!ok) break;
       int ks = take();
       if (!ok) break;
-      issue_s(0, 0, ks);
+      issue_s(0, room, ks);
       if (x.ntiles == 2) issue_s(1, 1, ks);
       umma_commit_if(leader, ring_empty(ks));
-      if (nkv == 1) umma_commit_if(leader, q_empty);
+      if (nkv == 1) umma_commit_if(leader, q_empty(room));
       if (x.ntiles == 2) {
         for (int j = 0; ok && j < nkv; ++j) {
           int vs = -1;
@@ -220,7 +234,7 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
               issue_s(t, t, ks);
               if (t == 1) {
                 umma_commit_if(leader, ring_empty(ks));
-                if (j + 2 == nkv) umma_commit_if(leader, q_empty);
+                if (j + 2 == nkv) umma_commit_if(leader, q_empty(room));
               }
             }
           }
@@ -229,9 +243,9 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
         if (nkv > 1) {
           ks = take();
           if (!ok) break;
-          issue_s(1, 0, ks);
+          issue_s(1, room, ks);
           umma_commit_if(leader, ring_empty(ks));
-          if (nkv == 2) umma_commit_if(leader, q_empty);
+          if (nkv == 2) umma_commit_if(leader, q_empty(room));
         }
         for (int j = 0; ok && j < nkv; ++j) {
           const int t = j & 1;
@@ -242,9 +256,9 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
           if (j + 2 < nkv) {
             ks = take();
             if (!ok) break;
-            issue_s(t, 0, ks);
+            issue_s(t, room, ks);
             umma_commit_if(leader, ring_empty(ks));
-            if (j + 3 == nkv) umma_commit_if(leader, q_empty);
+            if (j + 3 == nkv) umma_commit_if(leader, q_empty(room));
           }
         }
       }
@@ -252,127 +266,130 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
   } else if (warp < kManySoftmaxWarp) {
     // ------------------------------------------------------------------ operand tiles
     setmaxnreg_dec<kRegsDecode>();
-    const int dw = warp - 1, dt = static_cast<int>(threadIdx.x) - 32;
+    const bool query_warp = warp == kQueryWarp;
+    const int team = (warp - 1) >> 1, half = (warp - 1) & 1;
     // A lane decodes 32 values (one group) of a row at a time, eight neighbouring lanes eight neighbouring rows: the stores of a
-    // quarter of a warp then fall into eight different 16-byte columns of the swizzled tile.  So a warp has kStep rows at a time; the
-    // kParts parts of a tile go round the seven warps, for the values from the other end.
-    constexpr int kPieces = D / 32, kStep = 32 / kPieces, kParts = kBlockKeys / kStep, kReps = (kParts + kDecodeWarps - 1) / kDecodeWarps;
-    const int piece = (lane >> 3) % kPieces, lrow = (lane & 7) + 8 * ((lane >> 3) / kPieces);
-    struct Codes {
-      uint4 w[kReps];
-      uint32_t s[kReps];
-    };
+    // quarter of a warp then fall into eight different 16-byte columns of the swizzled tile.  A warp has kStep rows at a time and 64
+    // rows of a tile.  (All warps on every tile spent more issue slots on waiting and arriving than on decoding.)
+    constexpr int kPieces = D / 32, kStep = 32 / kPieces, kReps = 64 / kStep;
+    const int piece = (lane >> 3) % kPieces, lrow = half * 64 + (lane & 7) + 8 * ((lane >> 3) / kPieces);
+    uint32_t column[4];                                   // where the lane's four words of a row go in the tile
+#pragma unroll
+    for (int n = 0; n < 4; ++n) column[n] = (piece >> 1) * kAtom + lrow * 128 + ((((piece & 1) * 4 + n) ^ (lane & 7)) * 16);
+    // and where its codes and scales come from (16-byte columns of 64 bytes of codes are swizzled by row / 2, of 32 bytes by row / 4)
+    const uint32_t code_at = lrow * (D / 2) + (piece ^ (D == 128 ? (lrow >> 1) & 3 : (lrow >> 2) & 1)) * 16, scale_at = Cfg::kCodeBytes + lrow * (D / kKv4Group) + piece;
     bool ok = true;
-    int slot = 0;
-    uint32_t phase = 0, q_units = 0, armed = 0, armed_par = 0;        // slots that a copy was requested into, and the parity of the last
+    unsigned base = 0;                                    // place of the unit's first tile among all that pass through the ring
+    uint32_t q_units = 0, armed = 0, armed_par = 0, q_armed = 0, q_armed_par = 0;     // slots that a copy was requested into, and the parity of the last
     for (int u = unit0; ok && u < p.units; u += unit_step) {
       const Unit x = unit_at(u);
       if (x.nkv == 0) continue;
       const bool dual = x.ntiles == 1;
-      const long long row0 = x.e * p.elem_stride + static_cast<long long>(x.h) * p.L_cap + x.kb0 * kBlockKeys;
-      const int left = x.keys - x.kb0 * kBlockKeys;       // rows of the unit from the first block here
-      auto part_of = [&](int v, int k) { return k * kDecodeWarps + (v ? kDecodeWarps - 1 - dw : dw); };
-      auto load = [&](int v, int j, int k, Codes &c) {    // block j, part k of this warp
-        const int part = part_of(v, k), key = j * kBlockKeys + part * kStep + lrow;
-        const bool there = part < kParts && key < left && j < x.nkv;
-        const uint8_t *codes = v ? p.v_codes : p.k_codes, *scales = v ? p.v_scales : p.k_scales;
-        c.w[k] = there ? __ldg(reinterpret_cast<const uint4 *>(codes + (row0 + key) * (D / 2)) + piece) : make_uint4(0, 0, 0, 0);
-        c.s[k] = there ? __ldg(scales + (row0 + key) * (D / kKv4Group) + piece) : 0u;
-      };
-      // Requests that bring block j to L2: a tile decoded is a tile's time until the next one is read, less than HBM takes.
-      auto fetch = [&](int v, int j) {
-        if (lane != 0 || dw != (v ? 0 : kDecodeWarps - 1) || j >= x.nkv) return;
-        const int n = min(kBlockKeys, ((left + 7) & ~7) - j * kBlockKeys);            // whole 16 bytes of scales; within the cache (L_cap % 8 == 0)
-        const long long at = row0 + j * kBlockKeys;
-        l2_fetch((v ? p.v_codes : p.k_codes) + at * (D / 2), n * (D / 2));
-        l2_fetch((v ? p.v_scales : p.k_scales) + at * (D / kKv4Group), n * (D / kKv4Group));
-      };
-      auto put = [&](int v, int j, Codes &c) {
-        ok = __all_sync(0xffffffffu, mbar_wait(ring_empty(slot), phase ^ 1u, p.status, abort_flag, wb));
-        if (!ok) return;
-        fetch(v, j + kFetchAhead);
-        const uint32_t tile = ring_smem + slot * Cfg::kTileBytes + (piece >> 1) * kAtom;
+      const int tiles = 2 * x.nkv;
+      if (query_warp) {
+        const uint32_t room = q_units % qrooms;
+        if (q_units >= qrooms) ok = __all_sync(0xffffffffu, mbar_wait(q_empty(room), (q_units / qrooms - 1) & 1u, p.status, abort_flag, wb));
+        if (!ok) break;
+        const uint32_t q_dst = q_smem + room * Cfg::kTileBytes;
+        if (p.q_tma) {
+          if (lane == 0) {
+            mbar_expect_tx(q_full(room), x.ntiles * Cfg::kTileBytes);
+            for (int t = 0; t < x.ntiles; ++t)
 #pragma unroll
-        for (int k = 0; k < kReps; ++k) {
-          if (part_of(v, k) >= kParts) continue;
-          const int row = part_of(v, k) * kStep + lrow;
-          const uint32_t s2 = kv4_scale2(c.s[k]), f2 = kv4_offset2(s2), w[4] = {c.w[k].x, c.w[k].y, c.w[k].z, c.w[k].w};
-          load(v, j + 1, k, c);                           // the next block's, into the registers that have just been read
-#pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            uint32_t o[4];
-            kv4_word(w[n], s2, f2, o);
-            const uint32_t chunk = ((piece & 1) * 4 + n) ^ (row & 7);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile + row * 128 + chunk * 16), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+              for (int a = 0; a < D / 64; ++a)
+                tma_load_4d(q_dst + t * Cfg::kTileBytes + a * kAtom, &tmQ, q_full(room), a * 64, x.h * G, fast_div(x.rho0 + t * kTileRows, p.div_g), x.e);
+            q_armed |= 1u << room;
+            q_armed_par = (q_armed_par & ~(1u << room)) | ((q_units / qrooms & 1u) << room);
           }
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(ring_full(slot));
-      };
-      Codes ck, cv;
-      if constexpr (CODES) {
-        for (int j = 1; j < kFetchAhead; ++j) fetch(0, j), fetch(1, j);
-#pragma unroll
-        for (int k = 0; k < kReps; ++k) load(0, 0, k, ck);
-#pragma unroll
-        for (int k = 0; k < kReps; ++k) load(1, 0, k, cv);
-      }
-      if (q_units > 0) ok = __all_sync(0xffffffffu, mbar_wait(q_empty, (q_units - 1) & 1u, p.status, abort_flag, wb));
-      if (!ok) break;
-      ++q_units;
-      constexpr int kLanes = D / 8;                       // 16-byte pieces of a query row; rows that are not there become zeros
-      for (int n = dt; n < x.ntiles * kTileRows * kLanes; n += 32 * kDecodeWarps) {
-        const int row = n / kLanes, ch = n % kLanes, rho = x.rho0 + row;
-        const bool there = rho < nrows;
-        const bf16 *src = p.q + (there ? (static_cast<long long>(x.e) * p.r + rho / G) * p.ldq + (x.h * G + rho % G) * D + ch * 8 : 0);
-        const uint32_t dst = q_smem + (row >> 7) * Cfg::kTileBytes + (ch >> 3) * kAtom + (row & 127) * 128 + ((ch ^ row) & 7) * 16;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-      }
-      // The first tile is decoded while the queries are on the way.
-      if constexpr (CODES) {
-        for (int i = 0; ok && i < 2 * x.nkv; ++i) {
-          int j, v;
-          item_at(i, x.nkv, dual, j, v);
-          if (v) put(1, j, cv);
-          else put(0, j, ck);
-          if (i == 0) {
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(q_full);
+        } else {
+          constexpr int kLanes = D / 8;                   // 16-byte pieces of a query row; rows that are not there become zeros
+#pragma unroll 4
+          for (int n = lane; n < x.ntiles * kTileRows * kLanes; n += 32) {
+            const int row = n / kLanes, ch = n % kLanes, rho = x.rho0 + row;
+            const bool there = rho < nrows;
+            const int i = fast_div(rho, p.div_g);
+            const bf16 *src = p.q + (there ? (static_cast<long long>(x.e) * p.r + i) * p.ldq + (x.h * G + rho - i * G) * D + ch * 8 : 0);
+            const uint32_t dst = q_dst + (row >> 7) * Cfg::kTileBytes + (ch >> 3) * kAtom + (row & 127) * 128 + ((ch ^ row) & 7) * 16;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
           }
-          if (++slot == NR) { slot = 0; phase ^= 1u; }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(q_full(room));
         }
-      } else {
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_full);
-        if (threadIdx.x == 32) {
-          for (int i = 0; ok && i < 2 * x.nkv; ++i) {
+        ++q_units;
+        if (CODES && lane == 0) {
+          for (int i = 0; i < tiles; ++i) {
             int j, v;
             item_at(i, x.nkv, dual, j, v);
-            ok = mbar_wait(ring_empty(slot), phase ^ 1u, p.status, abort_flag, wb);
+            const unsigned at = base + i;
+            const int slot = at % (NC ? NC : 1);
+            ok = mbar_wait(raw_empty(slot), ((at / (NC ? NC : 1)) & 1u) ^ 1u, p.status, abort_flag, wb);
             if (!ok) break;
-            mbar_expect_tx(ring_full(slot), Cfg::kTileBytes);
-#pragma unroll
-            for (int a = 0; a < D / 64; ++a)
-              tma_load_3d(ring_smem + slot * Cfg::kTileBytes + a * kAtom, v ? &tmV : &tmK, ring_full(slot), a * 64, (x.kb0 + j) * kBlockKeys, x.e * p.Hkv + x.h);
+            const int key = (x.kb0 + j) * kBlockKeys, n = min(kBlockKeys, ((x.keys + 7) & ~7) - key);     // rows of scales: whole 16 bytes; within the cache (L_cap % 8 == 0)
+            const uint32_t dst = raw_smem + slot * Cfg::kRawBytes;
+            mbar_expect_tx(raw_full(slot), Cfg::kCodeBytes + n * (D / kKv4Group));
+            tma_load_4d(dst, v ? &tmV : &tmK, raw_full(slot), 0, key, x.h, x.e);      // rows beyond L_cap become zeros; what nobody sees is masked
+            bulk_load(dst + Cfg::kCodeBytes, (v ? p.v_scales : p.k_scales) + (x.e * p.elem_stride + static_cast<long long>(x.h) * p.L_cap + key) * (D / kKv4Group),
+                      n * (D / kKv4Group), raw_full(slot));
             armed |= 1u << slot;
-            armed_par = (armed_par & ~(1u << slot)) | (phase << slot);
-            if (++slot == NR) { slot = 0; phase ^= 1u; }
+            armed_par = (armed_par & ~(1u << slot)) | (((at / (NC ? NC : 1)) & 1u) << slot);
           }
         }
-        ok = __all_sync(0xffffffffu, ok) != 0;            // the lane that requests may have given up: its warp goes on together or not at all
-      }
-    }
-    if (!CODES && threadIdx.x == 32 && !ok)               // let every copy that was requested land before the shared memory is released
-      for (int s = 0; s < NR; ++s)
-        if (armed >> s & 1u) {
-          const long long t0 = clock64();
-          while (!mbar_try_wait(ring_full(s), armed_par >> s & 1u) && clock64() - t0 < kWaitCycles) {}
+      } else if constexpr (CODES) {
+        const int first = static_cast<int>((kDecodeTeams + team - base % kDecodeTeams) % kDecodeTeams);
+        for (int i = first; i < tiles; i += kDecodeTeams) {
+          const unsigned at = base + i;
+          const int slot = at % NR, from = at % (NC ? NC : 1);
+          ok = __all_sync(0xffffffffu, mbar_wait(raw_full(from), (at / (NC ? NC : 1)) & 1u, p.status, abort_flag, wb) &&
+                                           mbar_wait(ring_empty(slot), ((at / NR) & 1u) ^ 1u, p.status, abort_flag, wb));
+          if (!ok) break;
+          const uint32_t tile = ring_smem + slot * Cfg::kTileBytes, raw = raw_smem + from * Cfg::kRawBytes;
+#pragma unroll
+          for (int k = 0; k < kReps; ++k) {
+            const float4 c = ld_shared_f4(raw + code_at + k * kStep * (D / 2));
+            const uint32_t s2 = kv4_scale2(ld_shared_u8(raw + scale_at + k * kStep * (D / kKv4Group))), f2 = kv4_offset2(s2);
+            const uint32_t c4[4] = {__float_as_uint(c.x), __float_as_uint(c.y), __float_as_uint(c.z), __float_as_uint(c.w)};
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              uint32_t o[4];
+              kv4_word(c4[n], s2, f2, o);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile + column[n] + k * kStep * 128), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(ring_full(slot));
+            mbar_arrive(raw_empty(from));
+          }
         }
+      } else if (threadIdx.x == 32) {
+        for (int i = 0; ok && i < tiles; ++i) {
+          int j, v;
+          item_at(i, x.nkv, dual, j, v);
+          const unsigned at = base + i;
+          const int slot = at % NR;
+          ok = mbar_wait(ring_empty(slot), ((at / NR) & 1u) ^ 1u, p.status, abort_flag, wb);
+          if (!ok) break;
+          mbar_expect_tx(ring_full(slot), Cfg::kTileBytes);
+#pragma unroll
+          for (int a = 0; a < D / 64; ++a)
+            tma_load_3d(ring_smem + slot * Cfg::kTileBytes + a * kAtom, v ? &tmV : &tmK, ring_full(slot), a * 64, (x.kb0 + j) * kBlockKeys, x.e * p.Hkv + x.h);
+          armed |= 1u << slot;
+          armed_par = (armed_par & ~(1u << slot)) | (((at / NR) & 1u) << slot);
+        }
+      }
+      ok = __all_sync(0xffffffffu, ok) != 0;              // one lane may have given up alone: a warp goes on together or not at all
+      base += tiles;
+    }
+    if (!ok && (lane == 0) && (query_warp || (!CODES && warp == 1))) {      // let every copy that was requested land before the shared memory is released
+      const long long t0 = clock64();
+      for (int s = 0; s < 2; ++s)
+        while ((q_armed >> s & 1u) && !mbar_try_wait(q_full(s), q_armed_par >> s & 1u) && clock64() - t0 < kWaitCycles) {}
+      for (int s = 0; s < (CODES ? NC : NR); ++s)
+        while ((armed >> s & 1u) && !mbar_try_wait(CODES ? raw_full(s) : ring_full(s), armed_par >> s & 1u) && clock64() - t0 < kWaitCycles) {}
+    }
   } else {
     // ------------------------------------------------------------------ softmax
     setmaxnreg_inc<kRegsRows>();
@@ -380,22 +397,28 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
     const uint32_t lane_addr = static_cast<uint32_t>(quad * 32) << 16;
     const uint32_t s_addr = tmem_base + lane_addr + t * kBlockKeys, o_addr = tmem_base + lane_addr + 256 + t * D;
     const float c = p.scale_log2;
-    uint32_t s_par = 0, o_base = 0, last_par = 0;         // o_base: commits to o_full(t) so far; last_par: a bit a stream
+    uint32_t s_par = 0, o_base = 0, last_par = 0, swap_par = 0;      // o_base: commits to o_full(t) so far; last_par: a bit a stream
     bool ok = true;
     for (int u = unit0; ok && u < p.units; u += unit_step) {
       const Unit x = unit_at(u);
       const bool dual = x.ntiles == 1;
       const int nblk = dual ? (x.nkv + 1 - t) >> 1 : x.nkv;
       const int rho = x.rho0 + (dual ? 0 : t * kTileRows) + row_local;
+      const bool idle = rho - lane >= nrows;              // no row of this warp is there: nothing to compute, but the products wait for it
       m_ref = kNoRowMax;
       l_run = 0.f;
       any_block = nblk > 0;
       int limit = 0;
-      if (rho < nrows) limit = p.limits ? min(p.limits[static_cast<long long>(x.e) * p.r + rho / G], x.keys) : x.keys;
+      if (rho < nrows) limit = p.limits ? min(p.limits[static_cast<long long>(x.e) * p.r + fast_div(rho, p.div_g)], x.keys) : x.keys;
       for (int j = 0; j < nblk; ++j) {
         ok = __all_sync(0xffffffffu, mbar_wait(s_full(t), s_par, p.status, abort_flag, wb));
         if (!ok) break;
         s_par ^= 1u;
+        if (idle) {
+          mbar_arrive(p_half(t));
+          mbar_arrive(p_full(t));
+          continue;
+        }
         tc_fence_after();
         const int valid = limit - (x.kb0 + (dual ? 2 * j + t : j)) * kBlockKeys;       // keys of this block that the row sees (>= 128: all)
         uint32_t v[4][32];
@@ -465,11 +488,12 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
         unpack_f2(add_f2(ls[0], ls[1]), l0, l1);
         l_run += l0 + l1;
       }
-      if (!ok) { final_ok = false; break; }
+      if (!ok) { final_ok = false; break; }               // the others run into the abort flag in their waits
       if (x.nkv == 0) {                                   // nobody of the unit sees a key (or no key of this range): no product has run
         if constexpr (!RANGES) {
           if (t < x.ntiles && rho < nrows) {
-            uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((static_cast<long long>(x.e) * p.r + rho / G) * p.H + x.h * G + rho % G) * D);
+            const int i = fast_div(rho, p.div_g);
+            uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((static_cast<long long>(x.e) * p.r + i) * p.H + x.h * G + rho - i * G) * D);
             for (int k = 0; k < D / 8; ++k) dst[k] = make_uint4(0, 0, 0, 0);
           }
         }
@@ -486,10 +510,11 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
         float norm = 0.f, other = 0.f;
         if (dual) {
           asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(swap_smem + (t * kTileRows + row_local) * 8), "f"(m_ref), "f"(l_run) : "memory");
+          mbar_arrive(swap_full);
           if (t == 1 || both) ok = ok && __all_sync(0xffffffffu, mbar_wait(o_last(t ^ 1), last_par >> (t ^ 1) & 1u, p.status, abort_flag, wb));
-          ok = bar_and(1, 256, ok);
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(swap_full, swap_par, p.status, abort_flag, wb));
         }
-        if (ok) {
+        if (ok && !idle) {
           tc_fence_after();
           if (dual) {
             const float2 ml = ld_shared_f2(swap_smem + ((t ^ 1) * kTileRows + row_local) * 8);
@@ -503,8 +528,8 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
           }
           int u2 = u;                                     // decoded again: kept in registers through the loop, the unit spills
           asm volatile("" : "+r"(u2));
-          const int g2 = fast_div(u2, p.div_nqt), e2 = fast_div(g2, p.div_h), h2 = g2 - e2 * p.Hkv;
-          bf16 *dst = p.out + ((static_cast<long long>(e2) * p.r + rho / G) * p.H + h2 * G + rho % G) * D;
+          const int g2 = fast_div(u2, p.div_nqt), e2 = fast_div(g2, p.div_h), h2 = g2 - e2 * p.Hkv, i2 = fast_div(rho, p.div_g);
+          bf16 *dst = p.out + ((static_cast<long long>(e2) * p.r + i2) * p.H + h2 * G + rho - i2 * G) * D;
           const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0, there = rho < nrows;
           const int cc0 = dual ? t * (D / 64) : 0, cc1 = dual ? cc0 + D / 64 : D / 32;
 #pragma unroll 1
@@ -545,7 +570,12 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_
           tc_fence_before();
         }
         // both halves are out before either warp-group hands over a P of the next unit and so lets an accumulator be overwritten
-        if (dual) asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (dual) {
+          mbar_arrive(swap_done);
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(swap_done, swap_par, p.status, abort_flag, wb));
+          swap_par ^= 1u;
+        }
+        final_ok = ok;
       }
       last_par ^= dual ? (both ? 3u : 1u) : 3u;
     }
@@ -650,7 +680,7 @@ static cudaError_t many_prepare(int dev) {
   cudaError_t e = cudaFuncGetAttributes(&fa, attention_kv4_many_kernel<D, RANGES, CODES>);
   if (e != cudaSuccess) return e;
   if (fa.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
-  e = cudaFuncSetAttribute(attention_kv4_many_kernel<D, RANGES, CODES>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<D>::kSmemBytes);
+  e = cudaFuncSetAttribute(attention_kv4_many_kernel<D, RANGES, CODES>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<D, CODES>::kSmemBytes);
   if (e == cudaSuccess && dev < 64) prepared |= 1ull << dev;
   return e;
 }
@@ -677,7 +707,10 @@ static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, size_t bytes, i
   a.units = static_cast<int>(units);
   a.div_nqt = make_fast_div(static_cast<unsigned>(nqt), units);
   a.div_h = make_fast_div(a.Hkv, units);
-  CUtensorMap tk = {}, tv = {};
+  a.div_g = make_fast_div(G, rows + 256);
+  CUtensorMap tq = {}, tk = {}, tv = {};
+  a.q_tma = kTileRows % G == 0;                           // else the rows of a tile are no box
+  if (a.q_tma && !tmap_queries(&tq, a, kTileRows / G)) return cudaErrorInvalidValue;
   const size_t need = attention_kv4_workspace(a.B, a.Hkv, G, a.r, D, a.L);
   if (a.L > 0 && need > 0 && workspace && bytes >= need) {
     Kv4Args x = {};
@@ -696,19 +729,20 @@ static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, size_t bytes, i
     e = launch_kv4_rows(false, x, st);
     if (e == cudaSuccess) e = many_prepare<D, false, false>(dev);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attention_kv4_many_kernel<D, false, false>, dim3(a.units < num_sms ? a.units : num_sms), dim3(kManyThreads), ManyCfg<D>::kSmemBytes, st, tk, tv, a);
+    return launch_pdl(attention_kv4_many_kernel<D, false, false>, dim3(a.units < num_sms ? a.units : num_sms), dim3(kManyThreads), ManyCfg<D, false>::kSmemBytes, st, tq, tk, tv, a);
   }
+  if (!tmap_codes(&tk, a.k_codes, a, kBlockKeys) || !tmap_codes(&tv, a.v_codes, a, kBlockKeys)) return cudaErrorInvalidValue;
   if (a.kv_splits <= 1) {
     e = many_prepare<D, false, true>(dev);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attention_kv4_many_kernel<D, false, true>, dim3(a.units < num_sms ? a.units : num_sms), dim3(kManyThreads), ManyCfg<D>::kSmemBytes, st, tk, tv, a);
+    return launch_pdl(attention_kv4_many_kernel<D, false, true>, dim3(a.units < num_sms ? a.units : num_sms), dim3(kManyThreads), ManyCfg<D, true>::kSmemBytes, st, tq, tk, tv, a);
   }
   e = many_prepare<D, true, true>(dev);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.units * a.kv_splits);
   cfg.blockDim = dim3(kManyThreads);
-  cfg.dynamicSmemBytes = ManyCfg<D>::kSmemBytes;
+  cfg.dynamicSmemBytes = ManyCfg<D, true>::kSmemBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -718,7 +752,7 @@ static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, size_t bytes, i
   attr[1] = pdl_attribute();
   cfg.attrs = attr;
   cfg.numAttrs = one_predecessor(st) ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, attention_kv4_many_kernel<D, true, true>, tk, tv, a);
+  return cudaLaunchKernelEx(&cfg, attention_kv4_many_kernel<D, true, true>, tq, tk, tv, a);
 }
 
 cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {

@@ -89,6 +89,16 @@ bool tmap_codes(CUtensorMap *m, const void *codes, const Kv4AttnArgs &a, uint32_
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool tmap_queries(CUtensorMap *m, const Kv4AttnArgs &a, uint32_t rows) {
+  if (!tmap_init_driver()) return false;
+  cuuint64_t dims[4] = {static_cast<cuuint64_t>(a.D), static_cast<cuuint64_t>(a.H), static_cast<cuuint64_t>(a.r), static_cast<cuuint64_t>(a.B)};
+  cuuint64_t strides[3] = {static_cast<cuuint64_t>(a.D) * 2, static_cast<cuuint64_t>(a.ldq) * 2, static_cast<cuuint64_t>(a.ldq) * a.r * 2};
+  cuuint32_t box[4] = {64, static_cast<cuuint32_t>(a.H / a.Hkv), rows, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<bf16 *>(a.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 __device__ unsigned g_kernel_status;
 
 static std::string g_init_error;

@@ -320,11 +320,14 @@ struct Kv4AttnArgs {
   long long wait_cycles;                  // budget of every bounded wait (0: the default)
   // Filled by the launch functions: ranges of keys (a cluster's CTAs); query tiles a CTA, units and how they are numbered
   int kv_splits, tiles_per_cta, units;
-  FastDiv div_nqt, div_h;
+  FastDiv div_nqt, div_h, div_g;
+  int q_tma;                              // the queries come by TMA
 };
 // Codes of keys or values: {D / 2 bytes, L_cap rows, heads, elements}, a box of `rows` rows of one head, swizzled over its own row
 // length (64 bytes: 16-byte column ^= row / 2 mod 4; 32 bytes: ^= row / 4 mod 2).
 bool tmap_codes(CUtensorMap *m, const void *codes, const Kv4AttnArgs &a, uint32_t rows);
+// Queries: {D, H, r, B}, a box of 64 elements of the G heads of a group in `rows` rows.
+bool tmap_queries(CUtensorMap *m, const Kv4AttnArgs &a, uint32_t rows);
 // More than 16 query rows a cache head: tcgen05 (attention_kv4_many.cu).
 cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st);
 // Bytes of workspace that such a call can use (0: none).
