@@ -48,13 +48,14 @@ constexpr float kNoMax = -3.0e38f;
 // What a query row's share of a range of keys weighs; m in units of the scores, c of log2.  A range without any key has l = 0.
 __device__ __forceinline__ float range_weight(float m, float l, float m_all, float c) { return l == 0.f ? 0.f : exp2f((m - m_all) * c); }
 
+constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps;
+constexpr int kFewSets = 2;                               // sets of 16 keys that a warp takes of a stage
+constexpr int kFewKeys = 16 * kFewWarps, kFewStageKeys = kFewKeys * kFewSets;
 constexpr int kFewStages = 3;
 constexpr int kFewMaxRanges = 8;
 
-template <int D, int NB, int W>
+template <int D, int NB>
 struct FewCfg {
-  static constexpr int kFewSets = NB == 1 || W == 8 ? 2 : 1;                  // sets of 16 keys that a warp takes of a stage
-  static constexpr int kFewWarps = W, kFewThreads = 32 * W, kFewKeys = 16 * W, kFewStageKeys = kFewKeys * kFewSets;
   static constexpr int kRows = 8 * NB;                    // query rows of a unit
   static constexpr int kCodeBytes = kFewStageKeys * D / 2, kScaleBytes = kFewStageKeys * D / kKv4Group;
   static constexpr int kStageBytes = 2 * (kCodeBytes + kScaleBytes);          // K codes, V codes, K scales, V scales
@@ -68,10 +69,9 @@ struct FewCfg {
   static constexpr int kSmemBytes = kFrontBytes + kRecvBytes + kMlBytes + 128;
 };
 
-template <int D, int NB, int W>
-__global__ void __launch_bounds__(32 * W, NB == 1 ? 16 / W : 1) attention_kv4_few_kernel(const __grid_constant__ Kv4AttnArgs p) {
-  using Cfg = FewCfg<D, NB, W>;
-  constexpr int kFewWarps = W, kFewThreads = 32 * W, kFewKeys = Cfg::kFewKeys, kFewStageKeys = Cfg::kFewStageKeys, kFewSets = Cfg::kFewSets;
+template <int D, int NB>
+__global__ void __launch_bounds__(kFewThreads, NB == 1 ? 2 : 1) attention_kv4_few_kernel(const __grid_constant__ Kv4AttnArgs p) {
+  using Cfg = FewCfg<D, NB>;
   constexpr int KW = D / 32, VW = D / 64;                 // words a lane takes of a key row, of a value row
   extern __shared__ __align__(128) uint8_t smem_raw[];
   __shared__ uint64_t bars[kFewStages];
@@ -382,28 +382,19 @@ __global__ void __launch_bounds__(32 * W, NB == 1 ? 16 / W : 1) attention_kv4_fe
   }
 }
 
-int g_few_force = 0, g_few_w = 8;
-template <int D, int NB, int W>
-static cudaError_t launch_few(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
-  using Cfg = FewCfg<D, NB, W>;
-  constexpr int kFewThreads = 32 * W, kFewKeys = Cfg::kFewKeys;
+template <int D, int NB>
+static cudaError_t launch_few(const Kv4AttnArgs &a, cudaStream_t st) {
+  using Cfg = FewCfg<D, NB>;
   static unsigned long long prepared = 0;                 // a bit a device
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !(prepared >> dev & 1)) {
-    e = cudaFuncSetAttribute(attention_kv4_few_kernel<D, NB, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
+    e = cudaFuncSetAttribute(attention_kv4_few_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
     if (e != cudaSuccess) return e;
     if (dev < 64) prepared |= 1ull << dev;
   }
-  const int tiles = (a.r * (a.H / a.Hkv) + Cfg::kRows - 1) / Cfg::kRows;
-  const long long units = static_cast<long long>(tiles) * a.Hkv * a.B;
-  if (a.Hkv > 65535 || a.B > 65535) return cudaErrorInvalidConfiguration;
-  const int rounds = (a.L + kFewKeys - 1) / kFewKeys;
-  int s = 1;
-  while (s < kFewMaxRanges && units * s < 2 * num_sms && rounds >= 2 * (s * 2)) s *= 2;
-  if (g_few_force) s = g_few_force;
-  a.kv_splits = s;
+  const int tiles = (a.r * (a.H / a.Hkv) + Cfg::kRows - 1) / Cfg::kRows, s = a.kv_splits;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(tiles * s, a.Hkv, a.B);
   cfg.blockDim = dim3(kFewThreads);
@@ -420,15 +411,57 @@ static cudaError_t launch_few(Kv4AttnArgs a, int num_sms, cudaStream_t st) {
   if (one_predecessor(st)) attr[n++] = pdl_attribute();
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, attention_kv4_few_kernel<D, NB, W>, a);
+  return cudaLaunchKernelEx(&cfg, attention_kv4_few_kernel<D, NB>, a);
 }
 
-int g_few_rows = 16;
-cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {
-  if (a.r * static_cast<long long>(a.H / a.Hkv) > g_few_rows) return launch_attention_kv4_many(a, workspace, bytes, num_sms, st);
-  const bool one = a.r * static_cast<long long>(a.H / a.Hkv) <= 8;
-  if (a.D == 64) return one ? launch_few<64, 1, 8>(a, num_sms, st) : g_few_w == 12 ? launch_few<64, 2, 12>(a, num_sms, st) : launch_few<64, 2, 8>(a, num_sms, st);
-  return one ? launch_few<128, 1, 8>(a, num_sms, st) : g_few_w == 12 ? launch_few<128, 2, 12>(a, num_sms, st) : launch_few<128, 2, 8>(a, num_sms, st);
+// Waves of `ctas` blocks over `slots`: whole ones while there are fewer than `few`.
+static double waves_of(double ctas, double slots, double few) {
+  const double w = ctas / slots;
+  return w <= 1.0 ? 1.0 : w < few ? ceil(w) : w;
+}
+
+// Form, tiles and key ranges of a launch: the least estimated time (microseconds).  The estimates are fitted to forced launches on B200,
+// 10 shapes of few rows and 24 of many, 1 to 4096 rows over 77 to 10521 keys, which they rank as measured but for differences of a few
+// per cent.  Few rows: a block costs 5.5 and its keys 8.25 ns each at D = 128 with two blocks an SM, 4.5 with one (4.8 and 2.7 at D = 64);
+// 9 to 16 rows at a time, one block an SM, 5.8 (3.4).  Many rows: see attention_kv4_many_cost.  Where both can be taken they cross between 17 rows
+// (8 units: 11.5 us against 21.8) and 64 (32 units over 8000 keys: 52 against 29).
+Kv4Plan attention_kv4_plan(int B, int Hkv, int G, int r, int D, int L, int num_sms, const int *max_clusters) {
+  const long long rows = static_cast<long long>(r) * G, groups = static_cast<long long>(Hkv) * B;
+  Kv4Plan best = {kKv4Few, 1, 1};
+  double best_cost = 0.0;
+  auto take = [&](int form, int tiles, int splits, double cost) {
+    if (best_cost == 0.0 || cost < best_cost) { best = Kv4Plan{form, tiles, splits}; best_cost = cost; }
+  };
+  if (rows <= 64) {
+    const int nb = rows <= 8 ? 1 : 2, rounds = L > 0 ? (L + 127) / 128 : 1;
+    const double units = static_cast<double>((rows + 8 * nb - 1) / (8 * nb)) * groups, d = D == 128 ? 1.0 : 0.58;
+    for (int s = 1; s <= kFewMaxRanges; ++s) {
+      const int per = (rounds + s - 1) / s;
+      if (s > 1 && (rounds + per - 1) / per != s) continue;
+      const double ctas = units * s;
+      const double t = d * (nb == 2 ? 5.8e-3 : ctas <= num_sms / 2 ? 4.5e-3 : ctas <= num_sms ? 6.3e-3 : 8.25e-3);
+      take(kKv4Few, nb, s, waves_of(ctas, nb == 2 ? num_sms : 2 * num_sms, nb == 2 ? 4.0 : 3.0) * (5.5 + 0.25 * (s - 1) + per * 128 * t));
+    }
+  }
+  if (rows > 8)
+    for (int tiles = rows > 128 ? 2 : 1; tiles >= 1; --tiles)
+      for (int s = 1; s <= kKv4ManyMaxRanges; ++s) {
+        const double cost = attention_kv4_many_cost(rows, groups, D, L, tiles, s, num_sms, max_clusters);
+        if (cost > 0.0) take(kKv4Many, tiles, s, cost);
+      }
+  return best;
+}
+
+cudaError_t launch_attention_kv4(Kv4AttnArgs a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {
+  const int G = a.H / a.Hkv;
+  const int *clusters = attention_kv4_max_clusters();
+  if (!clusters) return cudaErrorInvalidConfiguration;
+  const Kv4Plan plan = attention_kv4_plan(a.B, a.Hkv, G, a.r, a.D, a.L, num_sms, clusters);
+  a.kv_splits = plan.splits;
+  a.tiles_per_cta = plan.tiles;
+  if (plan.form == kKv4Many) return launch_attention_kv4_many(a, workspace, bytes, num_sms, st);
+  if (a.D == 64) return plan.tiles == 1 ? launch_few<64, 1>(a, st) : launch_few<64, 2>(a, st);
+  return plan.tiles == 1 ? launch_few<128, 1>(a, st) : launch_few<128, 2>(a, st);
 }
 
 }  // namespace fvar

@@ -35,7 +35,6 @@ constexpr int kTileRows = 128, kBlockKeys = 128;
 constexpr int kAtom = 128 * 128;              // [128 rows][64 bf16], swizzled
 constexpr float kGrow = 8.0f;                 // log2 units
 constexpr float kNoRowMax = -3.0e38f;         // running maxima start here: finite, so that no difference of two of them is a NaN
-constexpr int kManyMaxRanges = 6;
 
 template <int D, bool CODES>
 struct ManyCfg {
@@ -685,10 +684,58 @@ static cudaError_t many_prepare(int dev) {
   return e;
 }
 
-int g_many_tiles = 0, g_many_splits = 0, g_many_pass = 0;
+// Estimated time in microseconds of a launch (0: not a launch): see attention_kv4_plan.  A block of 128 keys takes a lone tile 1.2 and a
+// pair 2.2 (1.0 and 1.75 at D = 64), a unit 3.5 or 4 more for its own first operands and store; ranges pay for their set-up, the
+// barriers and the rows that cross the cluster.  Pairs, which decode once for two tiles, win where lone tiles make another wave (1024 rows
+// of 2 x 16 heads over 4000 keys: 70 us against 82), lone tiles elsewhere (410 rows over 2931 keys: 35 against 56).
+double attention_kv4_many_cost(long long rows, long long groups, int D, int L, int tiles, int s, int num_sms, const int *max_clusters) {
+  const int nkv = (L + kBlockKeys - 1) / kBlockKeys, per = (nkv + s - 1) / s;
+  const double units = static_cast<double>((rows + tiles * kTileRows - 1) / (tiles * kTileRows)) * groups;
+  const double t_block = tiles == 2 ? (D == 128 ? 2.2 : 1.75) : (D == 128 ? 1.2 : 1.0);
+  if (s == 1) {
+    const double w = units / num_sms;
+    return 2.5 + (w <= 1.0 ? 1.0 : w < 8.0 ? ceil(w) : w) * ((tiles == 2 ? 4.0 : 3.5) + per * t_block);
+  }
+  if (per < 2 || (nkv + per - 1) / per != s || max_clusters[s] <= 0) return 0.0;             // at least two key blocks a range
+  const double part = (rows < tiles * kTileRows ? rows : tiles * kTileRows) / static_cast<double>(kTileRows);
+  return ceil(units / max_clusters[s]) * (7.0 + 0.8 * s + 3.0 * part + per * t_block);
+}
 
+// Resident clusters of s CTAs on the current device (0: none), for both widths: one CTA an SM.
+const int *attention_kv4_max_clusters() {
+  static int resident[64][kKv4ManyMaxRanges + 1];
+  static unsigned long long asked = 0;                    // a bit a device
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return nullptr;
+  if (asked >> dev & 1) return resident[dev];
+  if (many_prepare<128, true, true>(dev) != cudaSuccess) return nullptr;
+  for (int s = 1; s <= kKv4ManyMaxRanges; ++s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(s * 64);
+    cfg.blockDim = dim3(kManyThreads);
+    cfg.dynamicSmemBytes = ManyCfg<128, true>::kSmemBytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = s;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, attention_kv4_many_kernel<128, true, true>, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    resident[dev][s] = n;
+  }
+  asked |= 1ull << dev;
+  return resident[dev];
+}
+
+// Decoding once pays from about ten query tiles a head on (1600 rows over 4121 keys 122 -> 112 us, 4096 over 10521 639 -> 576; 1024 rows over
+// 4000 keys 70 -> 79).
 size_t attention_kv4_workspace(int B, int Hkv, int G, int r, int D, int L) {
-  if (g_many_pass ? g_many_pass < 0 : static_cast<long long>(r) * G <= 512) return 0;
+  if (static_cast<long long>(r) * G <= 1280) return 0;
   return static_cast<size_t>(B) * Hkv * L * D * 4;
 }
 
@@ -700,10 +747,11 @@ static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, size_t bytes, i
   const int G = a.H / a.Hkv;
   const long long rows = static_cast<long long>(a.r) * G;
   if (rows > INT_MAX - 256) return cudaErrorInvalidValue;
-  a.tiles_per_cta = g_many_tiles ? g_many_tiles : rows > kTileRows ? 2 : 1;
-  a.kv_splits = g_many_splits ? g_many_splits : 1;
+  const size_t need = attention_kv4_workspace(a.B, a.Hkv, G, a.r, D, a.L);
+  const bool decoded = a.L > 0 && need > 0 && workspace && bytes >= need;
+  if (decoded) a.tiles_per_cta = a.kv_splits = 1;         // lone tiles then (576 us against 603 of pairs)
   const long long nqt = (rows + a.tiles_per_cta * kTileRows - 1) / (a.tiles_per_cta * kTileRows), units = nqt * a.Hkv * a.B;
-  if (units * kManyMaxRanges > INT_MAX) return cudaErrorInvalidValue;
+  if (units * kKv4ManyMaxRanges > INT_MAX) return cudaErrorInvalidValue;
   a.units = static_cast<int>(units);
   a.div_nqt = make_fast_div(static_cast<unsigned>(nqt), units);
   a.div_h = make_fast_div(a.Hkv, units);
@@ -711,8 +759,7 @@ static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, size_t bytes, i
   CUtensorMap tq = {}, tk = {}, tv = {};
   a.q_tma = kTileRows % G == 0;                           // else the rows of a tile are no box
   if (a.q_tma && !tmap_queries(&tq, a, kTileRows / G)) return cudaErrorInvalidValue;
-  const size_t need = attention_kv4_workspace(a.B, a.Hkv, G, a.r, D, a.L);
-  if (a.L > 0 && need > 0 && workspace && bytes >= need) {
+  if (decoded) {
     Kv4Args x = {};
     x.k_out = static_cast<bf16 *>(workspace);
     x.v_out = x.k_out + static_cast<size_t>(a.B) * a.Hkv * a.L * D;

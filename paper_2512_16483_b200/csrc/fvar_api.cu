@@ -1803,6 +1803,7 @@ fvar_status fvar_attention_kv4(const void *q, long long ldq, const fvar_kv4 *cac
   if (!q || !out || H <= 0 || H % cache->n_heads || r <= 0 || L < 0 || L > cache->L_cap || ldq % 8 || ldq < static_cast<long long>(H) * cache->head_dim)
     return kfail(FVAR_EINVAL, "attention_kv4: bad arguments");
   if (off_grid(q, 16) || off_grid(out, 16) || off_grid(workspace, 16)) return kfail(FVAR_EINVAL, "attention_kv4: q, out and workspace must be 16-byte aligned");
+  if (cache->B > 65535 || cache->n_heads > 65535) return kfail(FVAR_EUNSUPPORTED, "attention_kv4: more than 65535 elements or heads");
   Kv4AttnArgs a = {};
   kv4_fields(cache, a);
   a.q = static_cast<const bf16 *>(q); a.ldq = ldq; a.H = H; a.Hkv = cache->n_heads; a.r = r; a.L = L; a.limits = limits;

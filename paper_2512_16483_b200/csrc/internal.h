@@ -318,7 +318,8 @@ struct Kv4AttnArgs {
   float scale_log2;                       // log2(e) / sqrt(D)
   unsigned *status;
   long long wait_cycles;                  // budget of every bounded wait (0: the default)
-  // Filled by the launch functions: ranges of keys (a cluster's CTAs); query tiles a CTA, units and how they are numbered
+  // Filled by launch_attention_kv4: ranges of keys (a cluster's CTAs), query tiles a CTA; by the launch of many rows: units and how they are
+  // numbered
   int kv_splits, tiles_per_cta, units;
   FastDiv div_nqt, div_h, div_g;
   int q_tma;                              // the queries come by TMA
@@ -328,11 +329,20 @@ struct Kv4AttnArgs {
 bool tmap_codes(CUtensorMap *m, const void *codes, const Kv4AttnArgs &a, uint32_t rows);
 // Queries: {D, H, r, B}, a box of 64 elements of the G heads of a group in `rows` rows.
 bool tmap_queries(CUtensorMap *m, const Kv4AttnArgs &a, uint32_t rows);
-// More than 16 query rows a cache head: tcgen05 (attention_kv4_many.cu).
+// Many query rows a cache head: tcgen05 (attention_kv4_many.cu).  workspace: see fvar_attention_kv4.
 cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st);
 // Bytes of workspace that such a call can use (0: none).
 size_t attention_kv4_workspace(int B, int Hkv, int G, int r, int D, int L);
-cudaError_t launch_attention_kv4(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st);
+// How a call is launched: few rows (8 or 16 at a time: tiles 1, 2) or many (lone tiles or pairs of 128 rows), in how many key ranges.
+enum Kv4Form { kKv4Few = 0, kKv4Many = 1 };
+struct Kv4Plan {
+  int form, tiles, splits;
+};
+constexpr int kKv4ManyMaxRanges = 6;
+Kv4Plan attention_kv4_plan(int B, int Hkv, int G, int r, int D, int L, int num_sms, const int *max_clusters);
+double attention_kv4_many_cost(long long rows, long long groups, int D, int L, int tiles, int s, int num_sms, const int *max_clusters);
+const int *attention_kv4_max_clusters();
+cudaError_t launch_attention_kv4(Kv4AttnArgs a, void *workspace, size_t bytes, int num_sms, cudaStream_t st);
 
 // Self-test of the bounded wait: one CTA waits on an mbarrier nobody signals with a budget of `cycles`, flags the
 // status word and returns.
