@@ -10,9 +10,9 @@ constexpr int kKv4Group = 32;                  // values a scale
 
 // bf16 pair (s, s) of a scale byte: 8 e + m moved to exponent e - 20 + 127 and the top three mantissa bits.
 __device__ __forceinline__ uint32_t kv4_scale2(uint32_t byte) { return byte * 0x00100010u + (107u << 7) * 0x00010001u; }
-// The pair (s of lo, s of hi).
-__device__ __forceinline__ uint32_t kv4_scales(uint32_t lo, uint32_t hi) { return hi * 0x00100000u + (lo * 16u + (107u << 7) * 0x00010001u); }
-
+// The same for two bytes, one in each half; with 2^100 besides.
+__device__ __forceinline__ uint32_t kv4_pairs(uint32_t bytes) { return bytes * 16u + (107u << 7) * 0x00010001u; }
+__device__ __forceinline__ uint32_t kv4_pairs_p(uint32_t bytes) { return bytes * 16u + (207u << 7) * 0x00010001u; }
 // The scale in byte g of four, as fp32.
 __device__ __forceinline__ float kv4_scale_f32(uint32_t bytes, int g) {
   return __uint_as_float(__byte_perm(bytes, 0, 0x4440 + g) * 0x00100000u + (107u << 23));

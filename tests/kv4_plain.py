@@ -33,17 +33,16 @@ def unpack(codes):
 
 
 def attention(q, K, V, L, limits=None):
-    """q [B][r][H * D], K, V [B][Hkv][>= L][D] -> (result, sum of weight x |value|, bound of a score's error), the first two
-    [B][r][H * D], the last [B][r][H].
+    """q [B][r][H * D], K, V [B][Hkv][>= L][D] -> (result [B][r][H * D], (sum of weight x |value|, sum of weight x 16 steps), bound of a
+    score's error [B][r][H]).
 
     A score is a sum of D products in fp32 of queries with the numbers u of the cache, 0 to 15, less 8 times the sum of the
     queries, times the groups' scales s: every term is at most 16 s |q|, and 16 s <= 16 / 7 of the group's greatest value (which is 7 s).
-    (D + 8) steps of 2^-23 of the sum of these, where a sum may be cut instead of rounded.  Where queries are split into two e4m3 terms
-    after scaling the row's greatest to at least 128, an element is off by half of e4m3's least step, 2^-10, at most: 2^-17 of the greatest."""
+    (D + 8) steps of 2^-23 of the sum of these, where a sum may be cut instead of rounded; the sums of the queries are taken in 24 bits."""
     B, r, _ = q.shape
     Hkv, D = K.shape[1], K.shape[3]
     H = q.shape[2] // D
-    out, mag, err = np.zeros((B, r, H, D)), np.zeros((B, r, H, D)), np.zeros((B, r, H))
+    out, mag, wide, err = np.zeros((B, r, H, D)), np.zeros((B, r, H, D)), np.zeros((B, r, H, D)), np.zeros((B, r, H))
     for b in range(B):
         n = np.full(r, L) if limits is None else np.clip(limits[b], 0, L)
         for h in range(H):
@@ -57,18 +56,19 @@ def attention(q, K, V, L, limits=None):
             w[some] /= w[some].sum(-1, keepdims=True)
             out[b, :, h], mag[b, :, h] = w @ v, w @ np.abs(v)
             if L:
-                steps = np.repeat(np.abs(k).reshape(L, -1, GROUP).max(-1), GROUP, -1) * (16.0 / 7.0)
-                err[b, :, h] = ((D + 8) * 2.0 ** -23 * (np.abs(x) @ steps.T).max(-1)
-                                + 2.0 ** -17 * np.abs(x).max(-1) * np.abs(k).sum(-1).max()) / np.sqrt(D)
-    return out.reshape(B, r, H * D), mag.reshape(B, r, H * D), err
+                steps = [np.repeat(np.abs(y).reshape(L, -1, GROUP).max(-1), GROUP, -1) * (16.0 / 7.0) for y in (k, v)]
+                wide[b, :, h] = w @ steps[1]
+                err[b, :, h] = (D + 8) * 2.0 ** -23 * (np.abs(x) @ steps[0].T).max(-1) / np.sqrt(D)
+    return out.reshape(B, r, H * D), (mag.reshape(B, r, H * D), wide.reshape(B, r, H * D)), err
 
 
-def bound(out, mag, err, L, D):
+def bound(out, mags, err, L, D):
     """How far a bf16 result of the kernels may be off.  With A = sum of weight x |value|: each weight is rounded to bf16 once
-    (2^-8 of A), the result once (2^-8 of it).  A score is off by err, then comes one product with log2(e) / sqrt(D), one
-    subtraction of the maximum (2^-23 of the scores each, within twice err) and an exp2 of 2^-22: every weight off by a factor within
-    1 +- (2 err + 2^-21), and the sum of the weights too.  The weighted sum itself has at most L / 8 + 64 steps (keys come eight or more
-    at a time, and ranges of keys are joined)."""
+    (2^-8 of A), for few rows once more after its product with a group's scale, and the result once (2^-8 of it).  A score is off by err, then
+    comes one product with log2(e) / sqrt(D), one subtraction of the maximum (2^-23 of the scores each, within twice err) and an exp2 of
+    2^-22: every weight off by a factor within 1 +- (2 err + 2^-21), and the sum of the weights too.  The weighted sum itself is the difference
+    of two sums of terms of at most 16 steps, in L / 8 + 64 steps (keys come eight or more at a time, and ranges of keys are joined)."""
+    mag, wide = mags
     e = np.repeat(err, mag.shape[-1] // err.shape[-1], -1)
-    rel = 2.0 ** -8 + 2 * (2 * e + 2.0 ** -21) + (L / 8 + 64) * 2.0 ** -23
-    return rel * mag + 2.0 ** -8 * (np.abs(out) + rel * mag) + 1e-30
+    off = (2 * 2.0 ** -8 + 2.0 ** -16 + 2 * (2 * e + 2.0 ** -21)) * mag + 2 * (L / 8 + 64) * 2.0 ** -23 * wide
+    return off + 2.0 ** -8 * (np.abs(out) + off) + 1e-30
