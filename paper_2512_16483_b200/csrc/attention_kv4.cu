@@ -14,7 +14,7 @@
 //                   the outputs' rows get 2^33 or 2^29 at the end.  All exact.
 //   keys' scales    a product covers one group of D and is multiplied by the group's scale when it is added to the score;
 //   values' scales  P is multiplied by the scales of a group before that group's product: one more rounding to bf16 of a weight;
-//   u - 8           - 8 scale (sum of the group's queries) is a small product of its own, scales x sums in three bf16 terms, and what the
+//   u - 8           - 8 scale (sum of the group's queries) is a small product of its own, scales x sums in two bf16 terms, and what the
 //                   scores begin with; 8 (sum of a group's P) is one more row of the second product, taken off at the end.
 // ldmatrix gives a key's group as a row (K) and, transposed, pairs of keys in a register (V), so nothing is shuffled.
 #include <float.h>
@@ -30,6 +30,11 @@ namespace fvar {
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// D[16][8] = A[16][8] B[8][8].
+__device__ __forceinline__ void mma_1688_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, {%7, %7, %7, %7};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
 }
 // D[16][8] = A[16][16] B[16][8].
 __device__ __forceinline__ void mma_16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -174,7 +179,8 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
   const int nst = (k1 - k0 + kFewStageKeys - 1) / kFewStageKeys;
   const long long row0 = b * p.elem_stride + static_cast<long long>(kv) * p.L_cap;
 
-  float o[NB][2 * NG][4], o8[NB][4];          // tiles 2 g, 2 g + 1: half-bytes 0, 2 and 1, 3 of group g; row g of o8: 8 x the group's sum of P
+  // Tiles 2 g and 2 g + 1: half-bytes 0, 2 and 1, 3 of group g.  o8: 8 x the sum of P of groups 2 t (its rows 0 - 7) and 2 t + 1 (8 - 15).
+  float o[NB][2 * NG][4], o8[NB][NG / 2][4];
   float m[NB][2], l[NB][2];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
@@ -183,7 +189,7 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[nb][t][k] = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o8[nb][k] = 0.f;
+    for (int k = 0; k < 2 * NG; ++k) o8[nb][k / 4][k % 4] = 0.f;
     m[nb][0] = m[nb][1] = kNoMax;
     l[nb][0] = l[nb][1] = 0.f;
   }
@@ -204,7 +210,7 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     // ------------------------------------------------------------------ queries
     // Lane (gid, tig) of a warp has word tig of every group of row gid: values 8 tig .. 8 tig + 7.  The row is multiplied by 2^sh so that
     // its greatest element is in [2^120, 2^121).
-    uint32_t q[NB][NG][4], sums[NB][2];                   // [pair of values]; the groups' sums x -8 2^-133, in the order of the small product
+    uint32_t q[NB][NG][4], sums[NB];                      // [pair of values]; the groups' sums x -8 2^-133, two terms of them
     float c[NB][2];                                       // of rows 2 tig, 2 tig + 1: from the products' units to those of log2
     int lim[NB][2];
 #pragma unroll
@@ -240,20 +246,12 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
         sum[g] = -sum[g] * k2m65 * k2m65;                 // - 8 2^-133 sum
       }
-      // Three bf16 terms of each sum (24 bits).  Row k of the second operand: D = 128: groups 0, 1 and 2, 3 of term 0, of term 1, of term 2;
-      // D = 64: groups 0, 1 of terms 0, 1, 2.
-      auto term = [&](float x, int n) {
-        for (int k = 0; k < n; ++k) x -= __bfloat162float(__float2bfloat16_rn(x));
-        return x;
-      };
-      if constexpr (NG == 4) {
-        const float x = tig & 1 ? sum[2] : sum[0], y = tig & 1 ? sum[3] : sum[1];
-        sums[nb][0] = pack_bf2(term(x, tig >> 1), term(y, tig >> 1));
-        sums[nb][1] = tig < 2 ? pack_bf2(term(x, 2), term(y, 2)) : 0u;
-      } else {
-        sums[nb][0] = tig < 3 ? pack_bf2(term(sum[0], tig), term(sum[1], tig)) : 0u;
-        sums[nb][1] = 0u;
-      }
+      // Two bf16 terms of each sum (16 bits; a score is off by 2^-14 of scale x sum |q| at most).  Row k of the small product's second operand:
+      // groups 0, 1 and 2, 3 of term 0, of term 1 (D = 64: groups 0, 1 of terms 0 and 1, zeros).
+      const float x = NG == 4 && (tig & 1) ? sum[NG - 2] : sum[0], y = NG == 4 && (tig & 1) ? sum[NG - 1] : sum[1];
+      const float xt = __bfloat162float(__float2bfloat16_rn(x)), yt = __bfloat162float(__float2bfloat16_rn(y));
+      const int term = NG == 4 ? tig >> 1 : tig;
+      sums[nb] = term == 0 ? pack_bf2(x, y) : term == 1 ? pack_bf2(x - xt, y - yt) : 0u;
       // 2^133 for the codes, 2^-sh for the queries; a row with an infinity or a NaN is NaN
       const float f = e == 255 ? __uint_as_float(0x7FC00000u) : fminf(p.scale_log2 * (k2p66 / f1) * ((2.f * k2p66) / f2), FLT_MAX);
 #pragma unroll
@@ -264,6 +262,13 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     }
     // ------------------------------------------------------------------ products
     const uint32_t pair_sel = (NG == 4 && (tig & 1)) ? 0x4342u : 0x4140u;     // scales of groups 2, 3 or 0, 1
+    // kept in registers: as constants they would be moved there again for every product
+    uint32_t upper[4], lower[4];                          // u = 8 in rows 0 - 7, in rows 8 - 15
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      asm volatile("mov.u32 %0, %1;" : "=r"(upper[k]) : "r"(k & 1 ? 0u : 0x00080008u));
+      asm volatile("mov.u32 %0, %1;" : "=r"(lower[k]) : "r"(k & 1 ? 0x00080008u : 0u));
+    }
     bool ok = true;
     for (int st = 0; st < nst; ++st) {
       const int slot = st % kFewStages;
@@ -291,7 +296,7 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
           }
           const uint32_t a0 = kv4_pairs(__byte_perm(ks[0], 0, pair_sel)), a1 = kv4_pairs(__byte_perm(ks[1], 0, pair_sel));
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) mma_16816_first(s[x][nb], a0, a1, a0, a1, sums[nb][0], sums[nb][1]);
+          for (int nb = 0; nb < NB; ++nb) mma_1688_first(s[x][nb], a0, a1, sums[nb]);
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
             const uint32_t w0 = w[0][g], w1 = w[1][g], v0 = w0 >> 8, v1 = w1 >> 8;
@@ -344,7 +349,11 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
               const float m2 = fmaxf(m[nb][i], t2), a = exp2f(m[nb][i] - m2);
               m[nb][i] = m2;
               l[nb][i] *= a;
-              o8[nb][i] *= a;
+#pragma unroll
+              for (int t = 0; t < NG / 2; ++t) {
+                o8[nb][t][i] *= a;
+                o8[nb][t][i + 2] *= a;
+              }
 #pragma unroll
               for (int t = 0; t < 2 * NG; ++t) {
                 o[nb][t][i] *= a;
@@ -388,11 +397,12 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
           }
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
-            const uint32_t w0 = w[0][g], w1 = w[1][g], v0 = w0 >> 8, v1 = w1 >> 8, eight = gid == g ? 0x00080008u : 0u;
+            const uint32_t w0 = w[0][g], w1 = w[1][g], v0 = w0 >> 8, v1 = w1 >> 8;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
               const uint32_t p0 = mul_bf2(pt[nb][0], sv[0][g]), p1 = mul_bf2(pt[nb][1], sv[1][g]);
-              mma_16816(o8[nb], eight, 0u, eight, 0u, p0, p1);
+              if (g & 1) mma_16816(o8[nb][g / 2], lower[0], lower[1], lower[2], lower[3], p0, p1);
+              else mma_16816(o8[nb][g / 2], upper[0], upper[1], upper[2], upper[3], p0, p1);
               mma_16816(o[nb][2 * g], w0 & kLow, v0 & kLow, w1 & kLow, v1 & kLow, p0, p1);
               mma_16816(o[nb][2 * g + 1], w0 & kHigh, v0 & kHigh, w1 & kHigh, v1 & kHigh, p0, p1);
             }
@@ -427,10 +437,10 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         const uint32_t dst = part + (warp * Cfg::kRows + row) * Cfg::kPitch + gid * 16;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const float eight = __shfl_sync(0xffffffffu, o8[nb][i], g * 4 + tig);
-          asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst + g * 128), "f"((o[nb][2 * g][i] - eight) * k2p33),
-                       "f"(fmaf(eight, -16.f, o[nb][2 * g + 1][i]) * k2p29), "f"((o[nb][2 * g][i + 2] - eight) * k2p33),
-                       "f"(fmaf(eight, -16.f, o[nb][2 * g + 1][i + 2]) * k2p29) : "memory");
+          const float off = o8[nb][g / 2][i + 2 * (g & 1)];
+          asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst + g * 128), "f"((o[nb][2 * g][i] - off) * k2p33),
+                       "f"(fmaf(off, -16.f, o[nb][2 * g + 1][i]) * k2p29), "f"((o[nb][2 * g][i + 2] - off) * k2p33),
+                       "f"(fmaf(off, -16.f, o[nb][2 * g + 1][i + 2]) * k2p29) : "memory");
         }
       }
   }
