@@ -552,8 +552,8 @@ static double waves_of(double ctas, double slots, double few) {
 
 // Form, tiles and key ranges of a launch: the least estimated time (microseconds).  The estimates are fitted to forced launches on B200,
 // 10 shapes of few rows and 24 of many, 1 to 4096 rows over 77 to 10521 keys, which they rank as measured but for differences of a few
-// per cent.  Few rows: a block costs 5.5 and its keys 8.25 ns each at D = 128 with two blocks an SM, 4.5 with one (4.8 and 2.7 at D = 64);
-// 9 to 16 rows at a time, one block an SM, 5.8 (3.4).  Many rows: see attention_kv4_many_cost.  Where both can be taken they cross between 17 rows
+// per cent.  Few rows: a block costs 5.5 and its keys 7.5 ns each at D = 128 with two blocks an SM, 4.1 with one (0.6 of that at D = 64);
+// 9 to 16 rows at a time, one block an SM, 6.1.  Many rows: see attention_kv4_many_cost.  Where both can be taken they cross between 17 rows
 // (8 units: 11.5 us against 21.8) and 64 (32 units over 8000 keys: 52 against 29).
 Kv4Plan attention_kv4_plan(int B, int Hkv, int G, int r, int D, int L, int num_sms, const int *max_clusters) {
   const long long rows = static_cast<long long>(r) * G, groups = static_cast<long long>(Hkv) * B;
@@ -564,12 +564,12 @@ Kv4Plan attention_kv4_plan(int B, int Hkv, int G, int r, int D, int L, int num_s
   };
   if (rows <= 64) {
     const int nb = rows <= 8 ? 1 : 2, rounds = L > 0 ? (L + 127) / 128 : 1;
-    const double units = static_cast<double>((rows + 8 * nb - 1) / (8 * nb)) * groups, d = D == 128 ? 1.0 : 0.58;
+    const double units = static_cast<double>((rows + 8 * nb - 1) / (8 * nb)) * groups, d = D == 128 ? 1.0 : 0.6;
     for (int s = 1; s <= kFewMaxRanges; ++s) {
       const int per = (rounds + s - 1) / s;
       if (s > 1 && (rounds + per - 1) / per != s) continue;
       const double ctas = units * s;
-      const double t = d * (nb == 2 ? 5.8e-3 : ctas <= num_sms / 2 ? 4.5e-3 : ctas <= num_sms ? 6.3e-3 : 8.25e-3);
+      const double t = d * (nb == 2 ? 6.1e-3 : ctas <= num_sms / 2 ? 4.1e-3 : ctas <= num_sms ? 5.7e-3 : 7.5e-3);
       take(kKv4Few, nb, s, waves_of(ctas, nb == 2 ? num_sms : 2 * num_sms, nb == 2 ? 4.0 : 3.0) * (5.5 + 0.25 * (s - 1) + per * 128 * t));
     }
   }
