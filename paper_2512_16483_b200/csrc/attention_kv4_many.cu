@@ -34,6 +34,9 @@ static_assert(2 * kRegsDecode + 2 * kRegsRows == 4 * kRegsLaunch, "what is given
 constexpr int kTileRows = 128, kBlockKeys = 128;
 constexpr int kAtom = 128 * 128;              // [128 rows][64 bf16], swizzled
 constexpr float kGrow = 8.0f;                 // log2 units
+// Maxima beyond this (log2 units) are taken off the scores before these are multiplied, not in the same operation: the product with the
+// maximum rounds by up to half a step, 2^-14 here, which all keys of a row share, but by any amount, up to an infinite weight, farther out.
+constexpr float kLargeMax = 1024.0f;
 constexpr float kNoRowMax = -3.0e38f;         // running maxima start here: finite, so that no difference of two of them is a NaN
 
 template <int D, bool CODES>
@@ -407,6 +410,7 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
       m_ref = kNoRowMax;
       l_run = 0.f;
       any_block = nblk > 0;
+      bool large = false;                                 // some row of the warp has a maximum beyond kLargeMax
       int limit = 0;
       if (rho < nrows) limit = p.limits ? min(p.limits[static_cast<long long>(x.e) * p.r + fast_div(rho, p.div_g)], x.keys) : x.keys;
       for (int j = 0; j < nblk; ++j) {
@@ -446,6 +450,7 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
           }
           const float alpha = need ? exp2f((m_ref - m_cand) * c) : 1.0f;
           if (need) m_ref = m_cand;
+          large = __any_sync(0xffffffffu, fabsf(m_ref) * c > kLargeMax && m_ref != kNoRowMax);
           l_run *= alpha;
           if (j > 0) {
 #pragma unroll 1
@@ -460,7 +465,14 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
             tmem_st_wait();
           }
         }
-        const float neg_mc = -m_ref * c;
+        float neg_mc = -m_ref * c;
+        if (large) {
+#pragma unroll
+          for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[cc][i] = __float_as_uint(__uint_as_float(v[cc][i]) - m_ref);
+          neg_mc = 0.f;
+        }
         const uint64_t c2 = pack_f2(c, c), neg_mc2 = pack_f2(neg_mc, neg_mc);
         uint64_t ls[2] = {0ull, 0ull};
 #pragma unroll
