@@ -424,7 +424,7 @@ fvar_status fvar_kv4_read(const fvar_kv4 *cache, int n, int L0, const int *start
  * keys and values are decoded once into it, which needs fvar_attention_kv4_workspace bytes; with less nothing is written there. */
 fvar_status fvar_attention_kv4(const void *q, long long ldq, const fvar_kv4 *cache, int H, int r, int L, const int *limits, void *out,
                                void *workspace, size_t workspace_bytes, void *stream);
-/* Bytes of workspace that the call above can use (0: none, or arguments that it refuses).  Host only. */
+/* Bytes of workspace with which the call above is faster on the current device (0: none, or arguments that it refuses).  Nothing is launched. */
 size_t fvar_attention_kv4_workspace(const fvar_kv4 *cache, int H, int r, int L);
 
 /* Failure-detection self-test: launches one CTA that waits, with a budget of `cycles` clock cycles, on a

@@ -551,16 +551,15 @@ static double waves_of(double ctas, double slots, double few) {
 }
 
 // Form, tiles and key ranges of a launch: the least estimated time (microseconds).  The estimates are fitted to forced launches on B200,
-// 10 shapes of few rows and 24 of many, 1 to 4096 rows over 77 to 10521 keys, which they rank as measured but for differences of a few
-// per cent.  Few rows: a block costs 5.5 and its keys 7.5 ns each at D = 128 with two blocks an SM, 4.1 with one (0.6 of that at D = 64);
+// 10 shapes of few rows and 24 of many, 1 to 5000 rows over 77 to 10521 keys: what they pick of the forms of many rows is 1 % slower than the
+// fastest on average and 7 % at worst.  Few rows: a block costs 5.5 and its keys 7.5 ns each at D = 128 with two blocks an SM, 4.1 with one (0.6 of that at D = 64);
 // 9 to 16 rows at a time, one block an SM, 6.1.  Many rows: see attention_kv4_many_cost.  Where both can be taken they cross between 17 rows
 // (8 units: 11.5 us against 21.8) and 64 (32 units over 8000 keys: 52 against 29).
 Kv4Plan attention_kv4_plan(int B, int Hkv, int G, int r, int D, int L, int num_sms, const int *max_clusters) {
   const long long rows = static_cast<long long>(r) * G, groups = static_cast<long long>(Hkv) * B;
-  Kv4Plan best = {kKv4Few, 1, 1};
-  double best_cost = 0.0;
+  Kv4Plan best = {kKv4Few, 1, 1, 0.f};
   auto take = [&](int form, int tiles, int splits, double cost) {
-    if (best_cost == 0.0 || cost < best_cost) { best = Kv4Plan{form, tiles, splits}; best_cost = cost; }
+    if (best.us == 0.f || cost < best.us) best = Kv4Plan{form, tiles, splits, static_cast<float>(cost)};
   };
   if (rows <= 64) {
     const int nb = rows <= 8 ? 1 : 2, rounds = L > 0 ? (L + 127) / 128 : 1;
@@ -576,10 +575,26 @@ Kv4Plan attention_kv4_plan(int B, int Hkv, int G, int r, int D, int L, int num_s
   if (rows > 8)
     for (int tiles = rows > 128 ? 2 : 1; tiles >= 1; --tiles)
       for (int s = 1; s <= kKv4ManyMaxRanges; ++s) {
-        const double cost = attention_kv4_many_cost(rows, groups, D, L, tiles, s, num_sms, max_clusters);
+        const double cost = attention_kv4_many_cost(rows, groups, D, L, tiles, s, false, num_sms, max_clusters);
         if (cost > 0.0) take(kKv4Many, tiles, s, cost);
       }
   return best;
+}
+
+// Query tiles a block where decoding the cache once first is estimated to take a twentieth less time than `plan` does; else 0.
+static int decode_once(const Kv4Plan &plan, int B, int Hkv, int G, int r, int D, int L, int num_sms, const int *max_clusters) {
+  if (plan.form != kKv4Many || L <= 0) return 0;
+  const long long rows = static_cast<long long>(r) * G, groups = static_cast<long long>(Hkv) * B;
+  const double one = attention_kv4_many_cost(rows, groups, D, L, 1, 1, true, num_sms, max_clusters);
+  const double two = rows > 128 ? attention_kv4_many_cost(rows, groups, D, L, 2, 1, true, num_sms, max_clusters) : one;
+  return 1.05 * fmin(one, two) < plan.us ? (one <= two ? 1 : 2) : 0;
+}
+
+size_t attention_kv4_workspace(int B, int Hkv, int G, int r, int D, int L, int num_sms) {
+  const int *clusters = attention_kv4_max_clusters();
+  if (!clusters) return 0;
+  return decode_once(attention_kv4_plan(B, Hkv, G, r, D, L, num_sms, clusters), B, Hkv, G, r, D, L, num_sms, clusters)
+             ? static_cast<size_t>(B) * Hkv * L * D * 4 : 0;
 }
 
 cudaError_t launch_attention_kv4(Kv4AttnArgs a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {
@@ -589,7 +604,17 @@ cudaError_t launch_attention_kv4(Kv4AttnArgs a, void *workspace, size_t bytes, i
   const Kv4Plan plan = attention_kv4_plan(a.B, a.Hkv, G, a.r, a.D, a.L, num_sms, clusters);
   a.kv_splits = plan.splits;
   a.tiles_per_cta = plan.tiles;
-  if (plan.form == kKv4Many) return launch_attention_kv4_many(a, workspace, bytes, num_sms, st);
+  if (plan.form == kKv4Many) {
+    if (workspace && bytes >= static_cast<size_t>(a.B) * a.Hkv * a.L * a.D * 4) {
+      const int tiles = decode_once(plan, a.B, a.Hkv, G, a.r, a.D, a.L, num_sms, clusters);
+      if (tiles) {
+        a.kv_splits = 1;
+        a.tiles_per_cta = tiles;
+        return launch_attention_kv4_many(a, workspace, num_sms, st);
+      }
+    }
+    return launch_attention_kv4_many(a, nullptr, num_sms, st);
+  }
   if (a.D == 64) return plan.tiles == 1 ? launch_few<64, 1>(a, st) : launch_few<64, 2>(a, st);
   return plan.tiles == 1 ? launch_few<128, 1>(a, st) : launch_few<128, 2>(a, st);
 }

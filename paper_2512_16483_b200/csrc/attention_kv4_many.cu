@@ -696,17 +696,18 @@ static cudaError_t many_prepare(int dev) {
   return e;
 }
 
-// Estimated time in microseconds of a launch (0: not a launch): see attention_kv4_plan.  A block of 128 keys takes a lone tile 1.2 and a
-// pair 2.2 (1.0 and 1.75 at D = 64), a unit 3.5 or 4 more for its own first operands and store; ranges pay for their set-up, the
-// barriers and the rows that cross the cluster.  Pairs, which decode once for two tiles, win where lone tiles make another wave (1024 rows
-// of 2 x 16 heads over 4000 keys: 70 us against 82), lone tiles elsewhere (410 rows over 2931 keys: 35 against 56).
-double attention_kv4_many_cost(long long rows, long long groups, int D, int L, int tiles, int s, int num_sms, const int *max_clusters) {
+// Estimated time in microseconds of a launch (0: not a launch): see attention_kv4_plan.  A block of 128 keys takes a lone tile 1.3 and a
+// pair 2.3 (1.13 and 2.0 at D = 64), decoded ones 1.05 and 1.95 (0.92 and 1.85); a unit takes 3.5 or 4 more for its own first operands and
+// store (0.5 less of decoded ones), the pass that decodes its bytes at 6.3 TB/s; ranges pay for their set-up, the barriers and the rows that
+// cross the cluster.  Pairs, which decode once for two tiles, win where lone tiles make another wave (1024 rows of 2 x 16 heads over 4000
+// keys: 70 us against 82), lone tiles elsewhere (410 rows over 2931 keys: 35 against 56).
+double attention_kv4_many_cost(long long rows, long long groups, int D, int L, int tiles, int s, bool decoded, int num_sms, const int *max_clusters) {
   const int nkv = (L + kBlockKeys - 1) / kBlockKeys, per = (nkv + s - 1) / s;
   const double units = static_cast<double>((rows + tiles * kTileRows - 1) / (tiles * kTileRows)) * groups;
-  const double t_block = tiles == 2 ? (D == 128 ? 2.2 : 1.75) : (D == 128 ? 1.2 : 1.0);
+  const double t_block = decoded ? (tiles == 2 ? (D == 128 ? 1.95 : 1.85) : (D == 128 ? 1.05 : 0.92)) : (tiles == 2 ? (D == 128 ? 2.3 : 2.0) : (D == 128 ? 1.3 : 1.13));
   if (s == 1) {
-    const double w = units / num_sms;
-    return 2.5 + (w <= 1.0 ? 1.0 : w < 8.0 ? ceil(w) : w) * ((tiles == 2 ? 4.0 : 3.5) + per * t_block);
+    const double w = units / num_sms, pass = decoded ? 3.0 + 0.8e-6 * groups * L * D : 0.0;
+    return 2.5 + pass + (w <= 1.0 ? 1.0 : w < 8.0 ? ceil(w) : w) * ((tiles == 2 ? 4.0 : 3.5) - (decoded ? 0.5 : 0.0) + per * t_block);
   }
   if (per < 2 || (nkv + per - 1) / per != s || max_clusters[s] <= 0) return 0.0;             // at least two key blocks a range
   const double part = (rows < tiles * kTileRows ? rows : tiles * kTileRows) / static_cast<double>(kTileRows);
@@ -744,24 +745,14 @@ const int *attention_kv4_max_clusters() {
   return resident[dev];
 }
 
-// Decoding once pays from about ten query tiles a head on (1600 rows over 4121 keys 122 -> 112 us, 4096 over 10521 639 -> 576; 1024 rows over
-// 4000 keys 70 -> 79).
-size_t attention_kv4_workspace(int B, int Hkv, int G, int r, int D, int L) {
-  if (static_cast<long long>(r) * G <= 1280) return 0;
-  return static_cast<size_t>(B) * Hkv * L * D * 4;
-}
-
 template <int D>
-static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {
+static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, int num_sms, cudaStream_t st) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const int G = a.H / a.Hkv;
   const long long rows = static_cast<long long>(a.r) * G;
   if (rows > INT_MAX - 256) return cudaErrorInvalidValue;
-  const size_t need = attention_kv4_workspace(a.B, a.Hkv, G, a.r, D, a.L);
-  const bool decoded = a.L > 0 && need > 0 && workspace && bytes >= need;
-  if (decoded) a.tiles_per_cta = a.kv_splits = 1;         // lone tiles then (576 us against 603 of pairs)
   const long long nqt = (rows + a.tiles_per_cta * kTileRows - 1) / (a.tiles_per_cta * kTileRows), units = nqt * a.Hkv * a.B;
   if (units * kKv4ManyMaxRanges > INT_MAX) return cudaErrorInvalidValue;
   a.units = static_cast<int>(units);
@@ -771,7 +762,7 @@ static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, size_t bytes, i
   CUtensorMap tq = {}, tk = {}, tv = {};
   a.q_tma = kTileRows % G == 0;                           // else the rows of a tile are no box
   if (a.q_tma && !tmap_queries(&tq, a, kTileRows / G)) return cudaErrorInvalidValue;
-  if (decoded) {
+  if (workspace) {                                        // decode the whole cache once, in a pass of its own
     Kv4Args x = {};
     x.k_out = static_cast<bf16 *>(workspace);
     x.v_out = x.k_out + static_cast<size_t>(a.B) * a.Hkv * a.L * D;
@@ -814,8 +805,8 @@ static cudaError_t launch_many_d(Kv4AttnArgs a, void *workspace, size_t bytes, i
   return cudaLaunchKernelEx(&cfg, attention_kv4_many_kernel<D, true, true>, tq, tk, tv, a);
 }
 
-cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st) {
-  return a.D == 64 ? launch_many_d<64>(a, workspace, bytes, num_sms, st) : launch_many_d<128>(a, workspace, bytes, num_sms, st);
+cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, int num_sms, cudaStream_t st) {
+  return a.D == 64 ? launch_many_d<64>(a, workspace, num_sms, st) : launch_many_d<128>(a, workspace, num_sms, st);
 }
 
 }  // namespace fvar

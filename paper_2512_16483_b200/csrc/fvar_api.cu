@@ -1794,7 +1794,9 @@ fvar_status fvar_kv4_read(const fvar_kv4 *cache, int n, int L0, const int *start
 
 size_t fvar_attention_kv4_workspace(const fvar_kv4 *cache, int H, int r, int L) {
   if (kv4_wrong(cache) || H <= 0 || H % cache->n_heads || r <= 0 || L <= 0 || L > cache->L_cap) return 0;
-  return attention_kv4_workspace(cache->B, cache->n_heads, H / cache->n_heads, r, cache->head_dim, L);
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  return attention_kv4_workspace(cache->B, cache->n_heads, H / cache->n_heads, r, cache->head_dim, L, sms);
 }
 
 fvar_status fvar_attention_kv4(const void *q, long long ldq, const fvar_kv4 *cache, int H, int r, int L, const int *limits, void *out,

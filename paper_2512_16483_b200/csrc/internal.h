@@ -329,18 +329,19 @@ struct Kv4AttnArgs {
 bool tmap_codes(CUtensorMap *m, const void *codes, const Kv4AttnArgs &a, uint32_t rows);
 // Queries: {D, H, r, B}, a box of 64 elements of the G heads of a group in `rows` rows.
 bool tmap_queries(CUtensorMap *m, const Kv4AttnArgs &a, uint32_t rows);
-// Many query rows a cache head: tcgen05 (attention_kv4_many.cu).  workspace: see fvar_attention_kv4.
-cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, size_t bytes, int num_sms, cudaStream_t st);
-// Bytes of workspace that such a call can use (0: none).
-size_t attention_kv4_workspace(int B, int Hkv, int G, int r, int D, int L);
+// Many query rows a cache head: tcgen05 (attention_kv4_many.cu).  With a workspace the cache is decoded into it first.
+cudaError_t launch_attention_kv4_many(const Kv4AttnArgs &a, void *workspace, int num_sms, cudaStream_t st);
+// Bytes of workspace that a call uses if it has them (0: none).
+size_t attention_kv4_workspace(int B, int Hkv, int G, int r, int D, int L, int num_sms);
 // How a call is launched: few rows (8 or 16 at a time: tiles 1, 2) or many (lone tiles or pairs of 128 rows), in how many key ranges.
 enum Kv4Form { kKv4Few = 0, kKv4Many = 1 };
 struct Kv4Plan {
   int form, tiles, splits;
+  float us;                               // estimated time
 };
 constexpr int kKv4ManyMaxRanges = 6;
 Kv4Plan attention_kv4_plan(int B, int Hkv, int G, int r, int D, int L, int num_sms, const int *max_clusters);
-double attention_kv4_many_cost(long long rows, long long groups, int D, int L, int tiles, int s, int num_sms, const int *max_clusters);
+double attention_kv4_many_cost(long long rows, long long groups, int D, int L, int tiles, int s, bool decoded, int num_sms, const int *max_clusters);
 const int *attention_kv4_max_clusters();
 cudaError_t launch_attention_kv4(Kv4AttnArgs a, void *workspace, size_t bytes, int num_sms, cudaStream_t st);
 
