@@ -403,7 +403,7 @@ typedef struct {
  * columns of a wider matrix, such as the keys and values of a fused QKV product); 16-byte aligned.  start dev int32 [B] or
  * NULL (then L0 for every element); count dev int32 [B] or NULL (then n; values beyond [0, n] count as its ends).
  * Rows that would fall outside the cache are not written; with L0 that is FVAR_EINVAL, with start the next
- * fvar_poll_status(NULL) returns FVAR_EINVAL.  n == 0 does nothing. */
+ * fvar_poll_status(NULL) returns FVAR_EINVAL.  n == 0 does nothing (K and V may be NULL). */
 fvar_status fvar_kv4_write(const fvar_kv4 *cache, const void *K, const void *V, long long ld, int n, int L0, const int *start,
                            const int *count, void *stream);
 
@@ -419,7 +419,7 @@ fvar_status fvar_kv4_read(const fvar_kv4 *cache, int n, int L0, const int *start
  * cache head h / (H / n_heads).  Row i of element b sees the first min(L, limits[b][i]) rows of its element (limits dev int32
  * [B][r], negative ones count as 0; NULL: the first L rows for every query row).  limits express padded batches, causal rows
  * and the rows of several scales at once, each up to the end of its own scale.  A row that sees nothing becomes 0.
- * 0 <= L <= L_cap; r >= 1.
+ * 0 <= L <= L_cap; r >= 1; more than 65535 elements or cache heads are FVAR_EUNSUPPORTED.
  * workspace (dev, 16-byte aligned, workspace_bytes long, used until the call's kernels have run; may be NULL): many query rows are faster when the
  * keys and values are decoded once into it, which needs fvar_attention_kv4_workspace bytes; with less nothing is written there. */
 fvar_status fvar_attention_kv4(const void *q, long long ldq, const fvar_kv4 *cache, int H, int r, int L, const int *limits, void *out,

@@ -1775,7 +1775,7 @@ static fvar_status kv4_rows(bool write, const fvar_kv4 *cache, Kv4Args &a, int n
 fvar_status fvar_kv4_write(const fvar_kv4 *cache, const void *K, const void *V, long long ld, int n, int L0, const int *start,
                            const int *count, void *stream) {
   if (const char *why = kv4_wrong(cache)) return kfail(FVAR_EINVAL, why);
-  if (!K || !V || ld % 8 || ld < static_cast<long long>(cache->n_heads) * cache->head_dim) return kfail(FVAR_EINVAL, "kv4_write: bad rows");
+  if ((n > 0 && (!K || !V)) || ld % 8 || ld < static_cast<long long>(cache->n_heads) * cache->head_dim) return kfail(FVAR_EINVAL, "kv4_write: bad rows");
   if (off_grid(K, 16) || off_grid(V, 16)) return kfail(FVAR_EINVAL, "kv4_write: K and V must be 16-byte aligned");
   Kv4Args a = {};
   a.k_rows = static_cast<const bf16 *>(K); a.v_rows = static_cast<const bf16 *>(V); a.ld = ld;
@@ -1784,7 +1784,7 @@ fvar_status fvar_kv4_write(const fvar_kv4 *cache, const void *K, const void *V, 
 
 fvar_status fvar_kv4_read(const fvar_kv4 *cache, int n, int L0, const int *start, const int *count, void *K_out, void *V_out, void *stream) {
   if (const char *why = kv4_wrong(cache)) return kfail(FVAR_EINVAL, why);
-  if (!K_out || !V_out) return kfail(FVAR_EINVAL, "kv4_read: NULL output");
+  if (n > 0 && (!K_out || !V_out)) return kfail(FVAR_EINVAL, "kv4_read: NULL output");
   if (off_grid(K_out, 16) || off_grid(V_out, 16)) return kfail(FVAR_EINVAL, "kv4_read: K_out and V_out must be 16-byte aligned");
   Kv4Args a = {};
   a.k_out = static_cast<bf16 *>(K_out); a.v_out = static_cast<bf16 *>(V_out);

@@ -221,3 +221,15 @@ def test_queries_of_any_magnitude(fv, r):
             s = np.abs(bf16_to_numpy(got) - ref) - 2.0 ** -8 * np.abs(ref) - 1e-30
             assert (s <= 0).mean() > 0.999
     assert np.isfinite(base).all()
+
+
+@pytest.mark.gpu
+def test_calls_without_rows(fv):
+    kv = fv.Kv4.empty(2, 3, 40, 64)
+    none = torch.empty((2, 0, 192), dtype=torch.bfloat16, device="cuda")
+    fv.fvar_kv4_write(kv, none, none, 40)
+    K, V = fv.fvar_kv4_read(kv, 0, 40)
+    assert K.shape == V.shape == (2, 0, 192)
+    assert fv.fvar_kv4_read(kv, 0, 3, out=(none, none))[0] is none
+    with pytest.raises(Exception):
+        fv.fvar_attention_kv4(none, kv, 8)

@@ -97,3 +97,21 @@ def test_binding_refuses_host_tensors():
     t = [torch.zeros((1, 2, 8, d), dtype=torch.uint8) for d in (32, 32, 2, 2)]
     with pytest.raises(AssertionError):
         fv.Kv4(*t)
+
+
+def test_no_rows_are_nothing():
+    """Tensors without elements have no address."""
+    from paper_2512_16483_b200 import binding
+    lib = binding.load_library()
+    for L0 in (0, 7, 40):
+        assert lib.fvar_kv4_write(_cache(), None, None, 256, 0, L0, None, None, None) == binding.OK
+        assert lib.fvar_kv4_read(_cache(), 0, L0, None, None, None, None, None) == binding.OK
+    assert lib.fvar_kv4_write(_cache(), None, None, 256, 0, 41, None, None, None) == binding.EINVAL
+    assert lib.fvar_kv4_read(_cache(), 0, -1, None, None, None, None, None) == binding.EINVAL
+
+
+def test_more_elements_or_heads_than_a_grid_has():
+    from paper_2512_16483_b200 import binding
+    lib = binding.load_library()
+    assert lib.fvar_attention_kv4(P, 512, _cache(B=65536), 8, 1, 40, None, P, None, 0, None) == binding.EUNSUPPORTED
+    assert lib.fvar_attention_kv4(P, 64 * 65536, _cache(n_heads=65536), 65536, 1, 40, None, P, None, 0, None) == binding.EUNSUPPORTED
