@@ -17,6 +17,9 @@
 //   u - 8           - 8 scale (sum of the group's queries) is a small product of its own, scales x sums in two bf16 terms, and what the
 //                   scores begin with; 8 (sum of a group's P) is one more row of the second product, taken off at the end.
 // ldmatrix gives a key's group as a row (K) and, transposed, pairs of keys in a register (V), so nothing is shuffled.
+// One row of 37 x 8 heads over 10521 keys, D = 128 (424 MB): 82.5 us, 5.1 TB/s; 280 instructions for 16 keys, of which 156 on the ALU
+// pipe (66 % busy, issue slots 59 %, tensor pipe 37 %).  4 rows of 64 x 8 heads over 0 - 8191 keys: 75.6 us, 3.8 TB/s.  One row of 2 x 16
+// heads (46 MB): 17.3 us; 16 rows of 4 x 16 heads over 6441 keys: 26.1.
 #include <float.h>
 #include <limits.h>
 #include <math.h>
