@@ -323,6 +323,7 @@ struct Kv4AttnArgs {
   int kv_splits, tiles_per_cta, units;
   FastDiv div_nqt, div_h, div_g;
   int q_tma;                              // the queries come by TMA
+  int by_length;                          // elements are taken the longest first (see longest_first)
 };
 // Codes of keys or values: {D / 2 bytes, L_cap rows, heads, elements}, a box of `rows` rows of one head, swizzled over its own row
 // length (64 bytes: 16-byte column ^= row / 2 mod 4; 32 bytes: ^= row / 4 mod 2).

@@ -141,6 +141,28 @@ def _call(fv, q, kv, L, lim, work, nbytes):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,Hkv,G,r,L,D", [(128, 2, 1, 65, 150, 64), (129, 2, 1, 65, 150, 64), (33, 5, 1, 70, 300, 128), (3, 60, 1, 130, 140, 64), (2, 30, 3, 100, 400, 128)])
+@pytest.mark.parametrize("kind", ["shuffled", "equal", "last row sees least", "nothing but one"])
+def test_ragged_batches(fv, B, Hkv, G, r, L, D, kind):
+    """More units than there are processors: elements are walked by length, each gets its own rows."""
+    rng = np.random.default_rng(B + r)
+    kv, K, V = _stored(fv, rng, B, Hkv, L, D)
+    q = _queries(rng, B, r, Hkv * G * D)
+    limits = np.broadcast_to((L * rng.permutation(B) // max(B - 1, 1))[:, None], (B, r)).copy()
+    if kind == "equal":
+        limits[:] = L - 3
+    elif kind == "last row sees least":
+        limits[:, -1] = -7
+    elif kind == "nothing but one":
+        limits[:] = 0
+        limits[B // 2] = 2 ** 31 - 1
+    got = fv.fvar_attention_kv4(to_bf16_cuda(q), kv, L, torch.tensor(limits, dtype=torch.int32, device="cuda"))
+    _compare(got, q, K, V, L, limits)
+    assert bool((got[torch.tensor(limits <= 0)] == 0).all())
+    assert fv.kernel_poll_status() == fv.OK
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("B,Hkv,G,r,L,D", [(2, 2, 1, 9500, 515, 64), (1, 2, 3, 6340, 390, 128), (4, 8, 1, 3500, 260, 128), (4, 8, 1, 8200, 260, 64)])
 def test_the_cache_decoded_once(fv, B, Hkv, G, r, L, D):
     """Lone tiles and pairs: with the workspace that the library asks for, with one that is too small (left alone) and without any.  Every
