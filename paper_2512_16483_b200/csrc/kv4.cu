@@ -21,14 +21,22 @@ __device__ __forceinline__ uint32_t kv4_scale_byte(float top) {
   const int u = static_cast<int>((__float_as_uint(t) + 0x000FFFFFu) >> 20) - (107 << 3);      // exponent and three bits of mantissa
   return static_cast<uint32_t>(min(max(u, 0), 255));
 }
-// x / s rounded to the nearest integer, halves away from zero, and kept within +-7: the sum with 1.5 2^23 + 8 has u = 8 + that in its
-// last four bits.  |x| / s is a half-integer or at least 2^-9 away from one (x has eight bits, s four), so 1 / s taken larger by 2^-13
-// moves the halves, and nothing else, across; it also covers the rounding of 1 / s and of the product.
-constexpr float kCodeBase = 12582920.0f;                  // 1.5 2^23 + 8
-constexpr uint32_t kCodeBits = 0x4B400000u;               // its bits, less 8
-__device__ __forceinline__ uint32_t kv4_code(float x, float inv_s) {
-  return __float_as_uint(fminf(fmaxf(fmaf(x, inv_s, kCodeBase), kCodeBase - 7.f), kCodeBase + 7.f));
+// Magnitudes of two pairs: the greater ones (a NaN wins), the smaller ones with the first one's signs.
+__device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
 }
+__device__ __forceinline__ uint32_t clamp_abs2(uint32_t x, uint32_t top) {
+  uint32_t d;
+  asm("min.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(top));
+  return d;
+}
+// x / s rounded to the nearest integer, halves away from zero: x (1 / s) + 1.5 2^23 is rounded there.  |x| / s is a half-integer or at least
+// 2^-9 away from one (x has eight bits, s four), so 1 / s taken larger by 2^-13 moves the halves, and nothing else, across; it also
+// covers the error of 1 / s.  The four even and the four odd numbers are added up as fp32 integers, two at a time, in their places over
+// 2^23 + 0x8888 (8 in each place), whose last 16 bits are then the half-word.
+constexpr float kToInt = 12582912.0f, kCodeBase = 8388608.0f + 34952.0f;
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
 // NaN -> 0 in both halves.
@@ -91,22 +99,32 @@ __device__ __forceinline__ void kv4_write_rows(const Kv4Args &p, const Kv4Place 
 #pragma unroll
     for (int t = 0; t < kPasses; ++t) {
       uint32_t e[4] = {x[v][t].x, x[v][t].y, x[v][t].z, x[v][t].w};
-      // maxima of the bit patterns: ordered as the magnitudes are
-      uint32_t top2 = __vmaxu2(__vmaxu2(e[0] & 0x7FFF7FFFu, e[1] & 0x7FFF7FFFu), __vmaxu2(e[2] & 0x7FFF7FFFu, e[3] & 0x7FFF7FFFu));
+      uint32_t top2 = max_abs2(max_abs2(e[0], e[1]), max_abs2(e[2], e[3])) & 0x7FFF7FFFu;
       if (__any_sync(0xffffffffu, (top2 & 0xFFFFu) > 0x7F80u || top2 > 0x7F80FFFFu)) {       // a NaN in the warp: rarely
 #pragma unroll
         for (int k = 0; k < 4; ++k) e[k] = drop_nan2(e[k]);
-        top2 = __vmaxu2(__vmaxu2(e[0] & 0x7FFF7FFFu, e[1] & 0x7FFF7FFFu), __vmaxu2(e[2] & 0x7FFF7FFFu, e[3] & 0x7FFF7FFFu));
+        top2 = max_abs2(max_abs2(e[0], e[1]), max_abs2(e[2], e[3])) & 0x7FFF7FFFu;
       }
+      // bit patterns are ordered as the magnitudes are
       top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 1));
       top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 2));
       const uint32_t byte = kv4_scale_byte(fmaxf(bf_lo(top2), bf_hi(top2)));
-      const float inv_s = __frcp_rn(__uint_as_float((byte + (107u << 3)) << 20)) * (1.0f + 1.0f / 8192.0f);
       bytes |= byte << (8 * t);
-      uint32_t word = 0;                                  // modulo 2^32: what stands above the last four bits of a code is taken off as one
+      const uint32_t most = mul_bf2(kv4_scale2(byte), 0x40E040E0u);                          // 7 s: exact, and what is beyond it takes 7
+      float inv_s;
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv_s) : "f"(__uint_as_float((byte + (107u << 3)) << 20)));
+      inv_s *= 1.0f + 1.0f / 8192.0f;
+      const uint64_t inv2 = pack_f2(inv_s, inv_s), up2 = pack_f2(kToInt, kToInt), down2 = pack_f2(-kToInt, -kToInt);
+      uint64_t sum2 = pack_f2(kCodeBase, kCodeBase);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) word += (kv4_code(bf_lo(e[k]), inv_s) << (4 * k)) + (kv4_code(bf_hi(e[k]), inv_s) << (16 + 4 * k));
-      word -= kCodeBits * 0x11111111u;
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x = clamp_abs2(e[k], most);
+        const float place = static_cast<float>(1 << (4 * k));
+        sum2 = fma_f2(add_f2(fma_f2(pack_f2(bf_lo(x), bf_hi(x)), inv2, up2), down2), pack_f2(place, place), sum2);
+      }
+      float even, odd;
+      unpack_f2(sum2, even, odd);
+      const uint32_t word = __byte_perm(__float_as_uint(even), __float_as_uint(odd), 0x5410);
       if (row[t] >= 0) codes[static_cast<long long>(row[t]) * kLanes] = word;
     }
     // Rows side by side have their scales side by side: a lane gathers those of one row, 32 bytes a warp.  (A byte a group and
