@@ -7,6 +7,8 @@
     python microbench.py attention_one B H D r L   # four attention launches on one shape (for ncu)
     python microbench.py gemmk [single|pair|flex <width>]       # the same over K at fixed R x N: fixed cost and cost per K step
     python microbench.py attention
+    python microbench.py kv4         # the cache in 4 bits: rows written, read back, attended to
+    python microbench.py kv4_one B Hkv G D r L     # four launches of attention over such a cache on one shape (for ncu)
     python microbench.py memory      # score, LayerNorm + modulate, restoration fill, selection
     python microbench.py transition  # between two scale steps: codeword search, Up-accumulate, Down
 
@@ -161,6 +163,52 @@ def attention():
     assert fv.kernel_poll_status() == fv.OK
 
 
+def _kv4_states(B, Hkv, G, D, r, L, n):
+    for _ in range(n):
+        kv = fv.Kv4.empty(B, Hkv, L, D)
+        rows = torch.randn(B, L, Hkv * D, device="cuda").bfloat16()
+        fv.fvar_kv4_write(kv, rows, rows.flip(1), 0)
+        yield kv, rows, torch.randn(B, r, Hkv * G * D, device="cuda").bfloat16()
+
+
+def kv4():
+    """Rotating over states that together exceed L2 several times."""
+    for B, Hkv, G, D, r, L in [(2, 16, 1, 128, 1, 10521), (37, 8, 1, 128, 1, 10521), (64, 8, 4, 128, 1, 8191), (4, 16, 1, 128, 16, 6441), (64, 16, 1, 64, 1, 680),
+                               (32, 30, 1, 64, 85, 509), (2, 16, 1, 128, 410, 2931), (16, 16, 1, 64, 680, 680), (2, 16, 1, 128, 4096, 10521)]:
+        packed = 2 * B * Hkv * L * D * 17 // 32
+        states = list(_kv4_states(B, Hkv, G, D, r, L, min(12, max(2, -(-400_000_000 // packed)))))
+        k = [0]
+
+        def nxt():
+            k[0] += 1
+            return states[k[0] % len(states)]
+
+        def write():
+            kv, rows, _ = nxt()
+            fv.fvar_kv4_write(kv, rows, rows, 0)
+
+        def read(out=tuple(torch.empty_like(states[0][1]) for _ in range(2))):
+            fv.fvar_kv4_read(nxt()[0], L, 0, out=out)
+
+        def attend():
+            kv, _, q = nxt()
+            fv.fvar_attention_kv4(q, kv, L)
+
+        w, rd, at = _time(write, n=40), _time(read, n=40), _time(attend, n=40)
+        print("B=%d Hkv=%d G=%d D=%d r=%d L=%d (%.0f MB): written %.1f us %.0f GB/s  read %.1f us %.0f GB/s  attended to %.1f us %.0f GB/s %.1f TFLOP/s" % (
+            B, Hkv, G, D, r, L, packed / 1e6, w, (packed + 4.0 * B * Hkv * L * D) / w / 1e3, rd, (packed + 4.0 * B * Hkv * L * D) / rd / 1e3,
+            at, packed / at / 1e3, 4.0 * B * Hkv * G * D * r * L / at / 1e6), flush=True)
+    assert fv.kernel_poll_status() == fv.OK
+
+
+def kv4_one():
+    B, Hkv, G, D, r, L = (int(x) for x in sys.argv[2:8])
+    for kv, _, q in _kv4_states(B, Hkv, G, D, r, L, 4):
+        fv.fvar_attention_kv4(q, kv, L)
+    torch.cuda.synchronize()
+    print("launched 4 calls of attention over 4 bits B=%d Hkv=%d G=%d D=%d r=%d L=%d" % (B, Hkv, G, D, r, L))
+
+
 def memory():
     for B, M, C in [(2, 4096, 2048), (32, 4096, 2048), (32, 1600, 1024)]:
         xs = [torch.randn(B, M, C, device="cuda") for _ in range(2)]
@@ -224,4 +272,4 @@ def transition():
 if __name__ == "__main__":
     which = sys.argv[1] if len(sys.argv) > 1 else "gemm"
     {"gemm": gemm, "gemmk": gemmk, "attention": attention, "memory": memory, "transition": transition, "skinny": skinny,
-     "ksplit": ksplit, "skinny_one": skinny_one, "flex_one": flex_one, "attention_one": attention_one}[which]()
+     "ksplit": ksplit, "skinny_one": skinny_one, "flex_one": flex_one, "attention_one": attention_one, "kv4": kv4, "kv4_one": kv4_one}[which]()

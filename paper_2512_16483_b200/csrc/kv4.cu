@@ -3,8 +3,10 @@
 // Both are bound by memory.  A lane holds 8 values (16 bytes of bf16, one 32-bit word of codes), a head's row is D / 8 lanes,
 // the group's maximum is two shuffles over four lanes.  A warp takes kPasses x 32 / (D / 8) rows of one head, keys and values
 // at once, all loads first; consecutive warps take consecutive heads of the same rows, which lie side by side in the input.
-// 1600 rows of 2 x 16 heads, D = 128 (33 MB): write 11.9 us on its own with cold caches, read 7.4 behind it.  6425 rows of them read
-// (133 MB): 20.7 us, 6.4 TB/s.  1 to 256 rows of 32 x 30 heads, D = 64: 14.4 and 9.6 us.
+// 1600 rows of 2 x 16 heads, D = 128 (33 MB): write 10.4 us on its own with cold caches, read 7.4 behind it.  6425 rows of them read
+// (133 MB): 20.7 us, 6.4 TB/s.  1 to 256 rows of 32 x 30 heads, D = 64: 12.2 and 9.7 us.  10521 rows of 37 x 8 heads (2.0 GB): 332 and 320 us,
+// 6.1 and 6.3 TB/s (write: 422 us with comparisons and limits one value at a time).  Two passes a warp: 12 % slower writes at the large
+// sizes; blocks of 128: 4 %.
 #include "kv4.cuh"
 #include "ptx.cuh"
 #include "softmax.cuh"
