@@ -300,7 +300,7 @@ def fvar_attention(q: torch.Tensor, Kc: torch.Tensor, Vt: torch.Tensor, L: int) 
 class Kv4:
     """A cache of keys and values in 4 bits a value (format: include/fvar.h) over the caller's tensors: codes uint8
     [B][n_heads][L_cap][D / 2], scales uint8 [B][n_heads][L_cap][D / 32].  Views of some elements ([1::2]: the null-prompt ones
-    of CFG pairs) are caches too."""
+    of CFG pairs) are caches too; elements that share memory (an expanded tensor) are refused."""
 
     def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor):
         B, H, L_cap, half = k_codes.shape
@@ -311,6 +311,7 @@ class Kv4:
             assert tuple(t.shape) == (B, H, L_cap, d) and t[0].is_contiguous(), (tuple(t.shape), t.stride())
             rows = t.stride(0) // d if B > 1 else H * L_cap
             assert stride in (None, rows) and (B == 1 or t.stride(0) == rows * d), "elements are not equally far apart"
+            assert rows >= H * L_cap, "elements share memory"            # 0, of an expanded tensor, would stand for the library's default
             stride = rows
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales    # kept alive
         self.B, self.n_heads, self.L_cap, self.head_dim, self.device = B, H, L_cap, D, k_codes.device
