@@ -418,7 +418,8 @@ fvar_status fvar_kv4_read(const fvar_kv4 *cache, int n, int L0, const int *start
  * aligned and apart from each other; B and D are the cache's.  H is a multiple of the cache's n_heads; query head h reads
  * cache head h / (H / n_heads).  Row i of element b sees the first min(L, limits[b][i]) rows of its element (limits dev int32
  * [B][r], negative ones count as 0; NULL: the first L rows for every query row).  limits express padded batches, causal rows
- * and the rows of several scales at once, each up to the end of its own scale.  A row that sees nothing becomes 0.
+ * and the rows of several scales at once, each up to the end of its own scale.  A row that sees nothing becomes 0; one with a
+ * NaN or an infinity is NaN.  Products q k are fp32 numbers: where they pass 3e38 the row may be NaN.
  * 0 <= L <= L_cap; r >= 1; more than 65535 elements or cache heads are FVAR_EUNSUPPORTED.
  * workspace (dev, 16-byte aligned, workspace_bytes long, used until the call's kernels have run; may be NULL): many query rows are faster when the
  * keys and values are decoded once into it, which needs fvar_attention_kv4_workspace bytes; with less nothing is written there. */

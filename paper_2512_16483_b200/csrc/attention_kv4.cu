@@ -454,7 +454,8 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
   auto store = [&](int row, int d, const float4 &even, const float4 &odd, float l_all) {
     const int rho = rho0 + row;
     if (rho >= nrows || abort_flag != 0) return;
-    const float inv = l_all == 0.f ? 0.f : 1.0f / l_all;
+    // no weight at all: the row sees no key, or its scores are all minus infinity
+    const float inv = l_all != 0.f ? 1.0f / l_all : limit_of(rho) > 0 ? __uint_as_float(0x7FC00000u) : 0.f;
     *reinterpret_cast<uint4 *>(p.out + ((static_cast<long long>(b) * p.r + rho / G) * p.H + kv * G + rho % G) * D + d) =
         make_uint4(pack_bf2(even.x * inv, odd.x * inv), pack_bf2(even.y * inv, odd.y * inv), pack_bf2(even.z * inv, odd.z * inv), pack_bf2(even.w * inv, odd.w * inv));
   };

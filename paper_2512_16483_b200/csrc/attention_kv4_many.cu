@@ -84,6 +84,9 @@ __device__ __forceinline__ void longest_first(uint8_t *order, const int *limits,
   __syncthreads();
 }
 
+// 1 / l of a row that sees `limit` keys.  No weight at all: it sees none, or its scores are all minus infinity.
+__device__ __forceinline__ float inverse_sum(float l, int limit) { return l != 0.f ? 1.0f / l : limit > 0 ? __uint_as_float(0x7FC00000u) : 0.f; }
+
 template <int D, bool RANGES, bool CODES>
 __global__ void __launch_bounds__(kManyThreads, 1)
 attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Kv4AttnArgs p) {
@@ -564,11 +567,11 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
             const float2 ml = ld_shared_f2(swap_smem + ((t ^ 1) * kTileRows + row_local) * 8);
             const float m_all = fmaxf(m_ref, ml.x), w0 = exp2f((m_ref - m_all) * c), w1 = exp2f((ml.x - m_all) * c);
             const float l_all = t == 0 ? fmaf(l_run, w0, ml.y * w1) : fmaf(ml.y, w1, l_run * w0);   // the same sum on both sides
-            const float inv = l_all == 0.f ? 0.f : 1.0f / l_all;
+            const float inv = inverse_sum(l_all, limit);
             norm = w0 * inv;
             other = w1 * inv;
           } else {
-            norm = l_run == 0.f ? 0.f : 1.0f / l_run;
+            norm = inverse_sum(l_run, limit);
           }
           int u2 = u;                                     // decoded again: kept in registers through the loop, the unit spills
           asm volatile("" : "+r"(u2));
@@ -693,7 +696,7 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
         float w16 = ml.y == 0.f ? 0.f : exp2f((ml.x - m_all) * c), l_all = ml.y * w16;
 #pragma unroll
         for (int d = 8; d > 0; d >>= 1) l_all += __shfl_xor_sync(0xffffffffu, l_all, d);
-        w16 *= l_all == 0.f ? 0.f : 1.0f / l_all;
+        w16 *= inverse_sum(l_all, l_all != 0.f || !live ? 0 : p.limits ? p.limits[static_cast<long long>(x.e) * p.r + rho / G] : p.L);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int t2 = 0; t2 < parts; ++t2) {
           const float w = __shfl_sync(0xffffffffu, w16, t2, 16);
