@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as ct
 import importlib
+import operator
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -338,13 +339,18 @@ def _rows_of(t: torch.Tensor, device) -> int:
     return ld
 
 
+def _int32(v) -> int:
+    """A whole number for a C int: ctypes would cut one of more bits, its nearest is refused by the library."""
+    return max(-2 ** 31, min(2 ** 31 - 1, operator.index(v)))
+
+
 def _kv4_place(cache: Kv4, start, count):
     """(L0, start, count) of a call as the library takes them."""
     for t in (start, count):
         if isinstance(t, torch.Tensor):
             _dev(t, torch.int32)
             assert tuple(t.shape) == (cache.B,) and t.device == cache.device, (tuple(t.shape), t.device)
-    return (0, start.data_ptr(), _ptr(count)) if isinstance(start, torch.Tensor) else (int(start), None, _ptr(count))
+    return (0, start.data_ptr(), _ptr(count)) if isinstance(start, torch.Tensor) else (_int32(start), None, _ptr(count))
 
 
 def _current(device):
@@ -402,7 +408,7 @@ def fvar_attention_kv4(q: torch.Tensor, cache: Kv4, L: int, limits: Optional[tor
     if out is None:
         out = torch.empty((B, r, C), dtype=torch.bfloat16, device=q.device)
     assert tuple(_dev(out, torch.bfloat16).shape) == (B, r, C) and out.device == cache.device, tuple(out.shape)
-    lib, H = load_library(), C // cache.head_dim
+    lib, H, L = load_library(), C // cache.head_dim, _int32(L)
     n = lib.fvar_attention_kv4_workspace(cache._ref, H, r, L)
     work = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     _check_kernel(lib.fvar_attention_kv4(q.data_ptr(), ld, cache._ref, H, r, L, _ptr(limits), out.data_ptr(), _ptr(work), n, _stream()))

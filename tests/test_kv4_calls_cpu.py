@@ -46,3 +46,69 @@ def test_elements_apart_are_taken():
     for which, B, stride in ((slice(None), 6, 32), (slice(1, None, 2), 3, 64), (slice(0, 1), 1, 32), (slice(0, None, 5), 2, 160)):
         kv = _cache([t[which] for t in all_])
         assert (kv.B, kv._c.elem_stride) == (B, stride) and kv._c.k_codes == all_[0][which].data_ptr()
+
+
+FAR = (2 ** 32, 2 ** 32 + 3, 2 ** 31, -2 ** 32 + 1, 2 ** 63, -2 ** 70)
+
+
+class Recorder:
+    """The library's functions, which take their arguments as ctypes converts them and launch nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        real = getattr(fv_lib, name)
+
+        def call(*args):
+            self.calls.append((name, [a if t is not ct.c_int else ct.c_int(a).value for t, a in zip(real.argtypes, args)]))
+            return 0
+        return call
+
+
+fv_lib = fv.load_library()
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    """The general way of every call, with the library's functions recorded."""
+    rec = Recorder()
+    monkeypatch.setattr(fv, "load_library", lambda: rec)
+    monkeypatch.setattr(fv, "_native", lambda: type("None_", (), {n: staticmethod(lambda *a: None) for n in ("kv4_write", "kv4_read", "attention_kv4")}))
+    monkeypatch.setattr(fv, "_current", lambda device: None)
+    monkeypatch.setattr(fv, "_stream", lambda: 0)
+    return rec
+
+
+def _bf16(*shape):
+    return OnDevice(torch.zeros(shape, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("far", FAR)
+def test_numbers_beyond_32_bits_are_not_cut(recorded, far):
+    """What reaches the library is outside every cache, as the number that was given is."""
+    kv, rows = _cache(_arrays(2, 2, 16, 64)), _bf16(2, 3, 128)
+    fv.fvar_kv4_write(kv, rows, rows, far)
+    fv.fvar_kv4_read(kv, 3, far, out=(rows, rows))
+    fv.fvar_attention_kv4(rows, kv, far, out=_bf16(2, 3, 128))
+    L0s = [recorded.calls[0][1][5], recorded.calls[1][1][2]]
+    Ls = [a[5] for n, a in recorded.calls if n == "fvar_attention_kv4"] + [a[3] for n, a in recorded.calls if n == "fvar_attention_kv4_workspace"]
+    assert [n for n, _ in recorded.calls] == ["fvar_kv4_write", "fvar_kv4_read", "fvar_attention_kv4_workspace", "fvar_attention_kv4"]
+    for v in L0s + Ls:
+        assert (v > 2 ** 30) if far > 0 else (v < 0), v
+    # and the library refuses them (no rows: nothing would be launched)
+    for L0 in L0s:
+        assert fv_lib.fvar_kv4_write(ct.byref(fv._Kv4(4096, 4096, 4096, 4096, 2, 2, 64, 16, 0)), None, None, 128, 0, L0, None, None, None) == fv.EINVAL
+
+
+def test_positions_are_whole_numbers(recorded):
+    kv, rows = _cache(_arrays(2, 2, 16, 64)), _bf16(2, 3, 128)
+    for bad in (3.7, "3", None):
+        for call in (lambda: fv.fvar_kv4_write(kv, rows, rows, bad), lambda: fv.fvar_kv4_read(kv, 3, bad, out=(rows, rows)),
+                     lambda: fv.fvar_attention_kv4(rows, kv, bad, out=_bf16(2, 3, 128))):
+            with pytest.raises(TypeError):
+                call()
+    assert not recorded.calls
+    import numpy as np
+    fv.fvar_kv4_write(kv, rows, rows, np.int64(5))
+    assert recorded.calls[0][1][5] == 5
