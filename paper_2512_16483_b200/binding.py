@@ -326,7 +326,9 @@ class Kv4:
         return cls(*(torch.empty(shape + (d,), dtype=torch.uint8, device="cuda") for d in (head_dim // 2, head_dim // 2, head_dim // 32, head_dim // 32)))
 
     def elements(self, which: slice) -> "Kv4":
-        """The cache of some of the elements; nothing is copied."""
+        """The cache of some of the elements, a slice of them; nothing is copied."""
+        if not isinstance(which, slice):                     # a list would index a copy, whose rows nobody reads
+            raise TypeError("elements of a cache are taken by a slice, not by %r" % (which,))
         return Kv4(self.k_codes[which], self.v_codes[which], self.k_scales[which], self.v_scales[which])
 
 

@@ -112,3 +112,13 @@ def test_positions_are_whole_numbers(recorded):
     import numpy as np
     fv.fvar_kv4_write(kv, rows, rows, np.int64(5))
     assert recorded.calls[0][1][5] == 5
+
+
+def test_elements_are_never_copied():
+    """A list of elements would index copies, and rows written to them would be lost."""
+    kv = _cache(_arrays(4, 2, 16, 64))
+    for which in ([0, 2], (0, 2), torch.tensor([0, 2]), torch.tensor([True, False, True, False]), 1, None):
+        with pytest.raises(TypeError):
+            kv.elements(which)
+    some = kv.elements(slice(1, None, 2))
+    assert some.B == 2 and some.v_scales.data_ptr() == kv.v_scales[1].data_ptr()
