@@ -306,6 +306,7 @@ class Kv4:
     def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor):
         B, H, L_cap, half = k_codes.shape
         D = 2 * half
+        assert B > 0 and H > 0 and L_cap > 0 and D in (64, 128), "no cache of the shape %s" % (tuple(k_codes.shape),)
         stride = None
         for t, d in ((k_codes, half), (v_codes, half), (k_scales, D // 32), (v_scales, D // 32)):
             assert t.is_cuda and t.dtype == torch.uint8 and t.device == k_codes.device, (t.device, t.dtype)

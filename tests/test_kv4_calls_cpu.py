@@ -122,3 +122,14 @@ def test_elements_are_never_copied():
             kv.elements(which)
     some = kv.elements(slice(1, None, 2))
     assert some.B == 2 and some.v_scales.data_ptr() == kv.v_scales[1].data_ptr()
+
+
+def test_no_elements_or_heads_are_refused():
+    for shape in ((0, 2, 16, 64), (2, 0, 16, 64), (2, 2, 0, 64)):
+        with pytest.raises(AssertionError):
+            _cache(_arrays(*shape))
+    with pytest.raises(AssertionError):
+        _cache(_arrays(4, 2, 16, 64)).elements(slice(4, None))
+    for D in (16, 32, 96, 256):
+        with pytest.raises(AssertionError):
+            _cache(_arrays(2, 2, 16, D))
