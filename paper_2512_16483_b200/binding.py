@@ -396,10 +396,12 @@ def fvar_kv4_read(cache: Kv4, n: int, start, count: Optional[torch.Tensor] = Non
 
 
 def fvar_attention_kv4(q: torch.Tensor, cache: Kv4, L: int, limits: Optional[torch.Tensor] = None,
-                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+                       out: Optional[torch.Tensor] = None, workspace: bool = True) -> torch.Tensor:
     """q bf16 [B][r][H * D] over the first L rows of a cache in 4 bits (row i of element b over the first limits[b][i], int32
-    [B][r]) -> bf16 [B][r][H * D].  H may be a multiple of the cache's heads; q may be columns of a wider matrix."""
-    res = _native().attention_kv4(cache._at, cache._dev, q, L, limits, out)
+    [B][r]) -> bf16 [B][r][H * D].  H may be a multiple of the cache's heads; q may be columns of a wider matrix.
+    Very many query rows are faster with a workspace, the L rows of the whole cache in bf16 (4 B n_heads L D bytes): it is taken from torch's
+    allocator unless that has no room for it or workspace is False."""
+    res = _native().attention_kv4(cache._at, cache._dev, q, L, limits, out, bool(workspace))
     if res is not None:
         return _result(res)
     _current(cache.device)
@@ -412,8 +414,11 @@ def fvar_attention_kv4(q: torch.Tensor, cache: Kv4, L: int, limits: Optional[tor
         out = torch.empty((B, r, C), dtype=torch.bfloat16, device=q.device)
     assert tuple(_dev(out, torch.bfloat16).shape) == (B, r, C) and out.device == cache.device, tuple(out.shape)
     lib, H, L = load_library(), C // cache.head_dim, _int32(L)
-    n = lib.fvar_attention_kv4_workspace(cache._ref, H, r, L)
-    work = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    n, work = lib.fvar_attention_kv4_workspace(cache._ref, H, r, L) if workspace else 0, None
+    try:
+        work = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    except torch.OutOfMemoryError:                           # the call does not need it
+        n = 0
     _check_kernel(lib.fvar_attention_kv4(q.data_ptr(), ld, cache._ref, H, r, L, _ptr(limits), out.data_ptr(), _ptr(work), n, _stream()))
     return out
 

@@ -16,6 +16,7 @@
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/util/Exception.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/fvar.h"
@@ -270,14 +271,14 @@ PyObject *kv4_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// (cache, device, q, L, limits, out) -> out, which is made when it is None
+// (cache, device, q, L, limits, out, workspace: True or False) -> out, which is made when it is None
 PyObject *attention_kv4(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded([&]() -> PyObject * {
     Kv4Call k;
     int64_t ld = 0;
     int L = 0;
     const int *limits = nullptr;
-    if (n != 6 || !as_cache(a[0], a[1], &k)) return none();
+    if (n != 7 || !as_cache(a[0], a[1], &k)) return none();
     const at::Tensor *q = as_rows(a[2], k, &ld);
     if (!q || k.c->head_dim <= 0 || q->size(2) % k.c->head_dim || !as_int(a[3], &L) || !as_ints(a[4], k, q->size(0), q->size(1), &limits)) return none();
     const int r = static_cast<int>(q->size(1)), H = static_cast<int>(q->size(2) / k.c->head_dim);
@@ -289,9 +290,13 @@ PyObject *attention_kv4(PyObject *, PyObject *const *a, Py_ssize_t n) {
       out = plain(a[5], at::kBFloat16, 3);
       if (!out || !here(*out, k) || out->sizes() != q->sizes()) return none();
     }
-    const size_t bytes = fvar_attention_kv4_workspace(k.c, H, r, L);
+    size_t bytes = a[6] == Py_True ? fvar_attention_kv4_workspace(k.c, H, r, L) : 0;
     at::Tensor work;
-    if (bytes) work = empty_like_device(*q, {static_cast<int64_t>(bytes)}, at::kByte);
+    try {
+      if (bytes) work = empty_like_device(*q, {static_cast<int64_t>(bytes)}, at::kByte);
+    } catch (const c10::OutOfMemoryError &) {             // the call does not need it
+      bytes = 0;
+    }
     const void *qp = q->data_ptr();
     void *op = out->data_ptr(), *wp = bytes ? work.data_ptr() : nullptr, *st = stream();
     const fvar_status e = unlocked([&] { return fvar_attention_kv4(qp, ld, k.c, H, r, L, limits, op, wp, bytes, st); });

@@ -66,3 +66,47 @@ def test_a_row_whose_scores_are_all_minus_infinity_is_nan(fv, r, L, D):
     seen, far = V[0, 1, : int(limits[0, r - 1])], bf16_to_numpy(got[r - 1, 1])
     off = 2.0 ** -7 * np.abs(seen).max(0)                # weights and the result rounded to bf16
     assert bool(nan[r - 1, 1]) or np.all((far >= seen.min(0) - off) & (far <= seen.max(0) + off))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_attention_where_memory_for_a_workspace_is_short_or_declined(fv, monkeypatch, native):
+    """98 MB of workspace that the allocator may not take, or is not asked for: the call runs as the library does without one."""
+    B, H, D, L, r = 4, 16, 128, 3000, 3500
+    kv = fv.Kv4.empty(B, H, L, D)
+    rows = torch.randn((B, L, H * D), device="cuda").bfloat16()
+    fv.fvar_kv4_write(kv, rows, rows.flip(1), 0)
+    q = torch.randn((B, r, H * D), device="cuda").bfloat16()
+    lib = fv.load_library()
+    n = lib.fvar_attention_kv4_workspace(kv._ref, H, r, L)
+    assert n == 4 * B * H * L * D
+    without = torch.empty_like(q)
+    assert lib.fvar_attention_kv4(q.data_ptr(), H * D, kv._ref, H, r, L, None, without.data_ptr(), None, 0, torch.cuda.current_stream().cuda_stream) == fv.OK
+    out = torch.zeros_like(q)
+    del rows
+    if not native:
+        monkeypatch.setattr(fv, "_native", lambda: type("None_", (), {"attention_kv4": staticmethod(lambda *a: None)}))
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    before = torch.cuda.memory_allocated()
+
+    def peak():                                          # since the last look at it (a comparison takes memory too)
+        top = torch.cuda.max_memory_allocated()
+        same = torch.equal(out, without)
+        out.zero_()
+        torch.cuda.empty_cache()
+        torch.cuda.reset_peak_memory_stats()
+        return top - before, same
+
+    torch.cuda.reset_peak_memory_stats()
+    assert fv.fvar_attention_kv4(q, kv, L, out=out, workspace=False) is out
+    assert peak() == (0, True)
+    free, total = torch.cuda.mem_get_info()
+    torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + n // 2) / total)
+    try:
+        assert fv.fvar_attention_kv4(q, kv, L, out=out) is out
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert peak() == (0, True)
+    fv.fvar_attention_kv4(q, kv, L, out=out)
+    assert peak()[0] >= n
+    assert fv.kernel_poll_status() == fv.OK

@@ -133,3 +133,38 @@ def test_no_elements_or_heads_are_refused():
     for D in (16, 32, 96, 256):
         with pytest.raises(AssertionError):
             _cache(_arrays(2, 2, 16, D))
+
+
+class Wants(Recorder):
+    """A library that would like a workspace."""
+
+    def __getattr__(self, name):
+        call = super().__getattr__(name)
+        return call if name != "fvar_attention_kv4_workspace" else lambda *a: (call(*a), 4096)[1]
+
+
+def _attend_where_no_workspace_is_to_be_had(monkeypatch, **how):
+    rec, asked, real = Wants(), [], torch.empty
+    monkeypatch.setattr(fv, "load_library", lambda: rec)
+
+    def empty(*shape, dtype=None, device=None):
+        asked.append((shape, dtype))
+        if dtype == torch.uint8:
+            raise torch.OutOfMemoryError("CUDA out of memory")
+        return OnDevice(real(*shape, dtype=dtype))
+    monkeypatch.setattr(torch, "empty", empty)
+    kv, q = _cache(_arrays(2, 2, 16, 64)), _bf16(2, 3, 128)
+    out = fv.fvar_attention_kv4(q, kv, 16, **how)
+    assert tuple(out.shape) == (2, 3, 128)
+    (name, args), = [c for c in rec.calls if c[0] == "fvar_attention_kv4"]
+    assert args[8] is None and args[9] == 0              # no address, no bytes
+    return [shape for shape, dtype in asked if dtype == torch.uint8]
+
+
+def test_attention_without_memory_for_a_workspace(recorded, monkeypatch):
+    """The workspace makes a call faster and is not needed for it."""
+    assert _attend_where_no_workspace_is_to_be_had(monkeypatch) == [(4096,)]
+
+
+def test_a_workspace_can_be_declined(recorded, monkeypatch):
+    assert _attend_where_no_workspace_is_to_be_had(monkeypatch, workspace=False) == []
