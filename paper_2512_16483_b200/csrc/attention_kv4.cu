@@ -25,6 +25,7 @@
 #include <math.h>
 
 #include "kv4.cuh"
+#include "per_device.h"
 #include "ptx.cuh"
 
 namespace fvar {
@@ -517,15 +518,12 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 template <int D, int NB>
 static cudaError_t launch_few(const Kv4AttnArgs &a, cudaStream_t st) {
   using Cfg = FewCfg<D, NB>;
-  static unsigned long long prepared = 0;                 // a bit a device
+  static PerDevice prepared;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess)
+    e = prepared.once(dev, [] { return cudaFuncSetAttribute(attention_kv4_few_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes); });
   if (e != cudaSuccess) return e;
-  if (dev >= 64 || !(prepared >> dev & 1)) {
-    e = cudaFuncSetAttribute(attention_kv4_few_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) prepared |= 1ull << dev;
-  }
   CUtensorMap tk, tv;
   if (!tmap_codes(&tk, a.k_codes, a, kFewStageKeys) || !tmap_codes(&tv, a.v_codes, a, kFewStageKeys)) return cudaErrorInvalidValue;
   const int tiles = (a.r * (a.H / a.Hkv) + Cfg::kRows - 1) / Cfg::kRows, s = a.kv_splits;

@@ -25,6 +25,7 @@
 #include <math.h>
 
 #include "kv4.cuh"
+#include "per_device.h"
 #include "ptx.cuh"
 #include "softmax.cuh"
 
@@ -721,16 +722,15 @@ attention_kv4_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
 
 template <int D, bool RANGES, bool CODES>
 static cudaError_t many_prepare(int dev) {
-  static unsigned long long prepared = 0;                 // a bit a device
-  if (dev < 64 && (prepared >> dev & 1)) return cudaSuccess;
-  // The register split draws on what the block was launched with: refuse a build whose kernel got fewer.
-  cudaFuncAttributes fa;
-  cudaError_t e = cudaFuncGetAttributes(&fa, attention_kv4_many_kernel<D, RANGES, CODES>);
-  if (e != cudaSuccess) return e;
-  if (fa.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
-  e = cudaFuncSetAttribute(attention_kv4_many_kernel<D, RANGES, CODES>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<D, CODES>::kSmemBytes);
-  if (e == cudaSuccess && dev < 64) prepared |= 1ull << dev;
-  return e;
+  static PerDevice prepared;
+  return prepared.once(dev, [] {
+    // The register split draws on what the block was launched with: refuse a build whose kernel got fewer.
+    cudaFuncAttributes fa;
+    const cudaError_t e = cudaFuncGetAttributes(&fa, attention_kv4_many_kernel<D, RANGES, CODES>);
+    if (e != cudaSuccess) return e;
+    if (fa.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
+    return cudaFuncSetAttribute(attention_kv4_many_kernel<D, RANGES, CODES>, cudaFuncAttributeMaxDynamicSharedMemorySize, ManyCfg<D, CODES>::kSmemBytes);
+  });
 }
 
 // Estimated time in microseconds of a launch (0: not a launch): see attention_kv4_plan.  A block of 128 keys takes a lone tile 1.3 and a
@@ -753,33 +753,35 @@ double attention_kv4_many_cost(long long rows, long long groups, int D, int L, i
 
 // Resident clusters of s CTAs on the current device (0: none), for both widths: one CTA an SM.
 const int *attention_kv4_max_clusters() {
-  static int resident[64][kKv4ManyMaxRanges + 1];
-  static unsigned long long asked = 0;                    // a bit a device
+  static int resident[kMaxDevices][kKv4ManyMaxRanges + 1];
+  static PerDevice asked;
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return nullptr;
-  if (asked >> dev & 1) return resident[dev];
-  if (many_prepare<128, true, true>(dev) != cudaSuccess) return nullptr;
-  for (int s = 1; s <= kKv4ManyMaxRanges; ++s) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(s * 64);
-    cfg.blockDim = dim3(kManyThreads);
-    cfg.dynamicSmemBytes = ManyCfg<128, true>::kSmemBytes;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = s;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, attention_kv4_many_kernel<128, true, true>, &cfg) != cudaSuccess) {
-      cudaGetLastError();
-      n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= kMaxDevices) return nullptr;
+  const cudaError_t e = asked.once(dev, [dev] {
+    const cudaError_t e = many_prepare<128, true, true>(dev);
+    if (e != cudaSuccess) return e;
+    for (int s = 1; s <= kKv4ManyMaxRanges; ++s) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(s * 64);
+      cfg.blockDim = dim3(kManyThreads);
+      cfg.dynamicSmemBytes = ManyCfg<128, true>::kSmemBytes;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = s;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      int n = 0;
+      if (cudaOccupancyMaxActiveClusters(&n, attention_kv4_many_kernel<128, true, true>, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+      }
+      resident[dev][s] = n;
     }
-    resident[dev][s] = n;
-  }
-  asked |= 1ull << dev;
-  return resident[dev];
+    return cudaSuccess;
+  });
+  return e == cudaSuccess ? resident[dev] : nullptr;
 }
 
 template <int D>

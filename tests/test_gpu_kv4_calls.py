@@ -1,4 +1,8 @@
 """Calls of the cache in 4 bits at the edges of what they allow, in every kind of launch."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -8,6 +12,8 @@ import synth_inputs as si
 from helpers import bf16_to_numpy, to_bf16_cuda
 
 pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 # r, L and whether the cache is decoded once for them: few rows on one range and several, lone tiles and pairs, alone and in ranges
 LAUNCHES = [(1, 77), (3, 3000), (12, 77), (12, 3000), (70, 77), (70, 2100), (300, 140), (129, 6441), (9500, 515)]
@@ -110,3 +116,36 @@ def test_attention_where_memory_for_a_workspace_is_short_or_declined(fv, monkeyp
     fv.fvar_attention_kv4(q, kv, L, out=out)
     assert peak()[0] >= n
     assert fv.kernel_poll_status() == fv.OK
+
+
+FIRST_CALLS = """
+import threading
+import torch
+from paper_2512_16483_b200 import binding as fv
+fv.load_library(), fv._native()
+torch.manual_seed(0)
+kv = fv.Kv4.empty(2, 4, 515, 64)
+rows = torch.randn(2, 515, 256, device="cuda").bfloat16()
+fv.fvar_kv4_write(kv, rows, rows.flip(1), 0)
+qs = [torch.randn(2, r, 256, device="cuda").bfloat16() for r in (1, 12, 70, 130, 9500, 1, 12, 70)]
+torch.cuda.synchronize()
+gate, outs = threading.Barrier(len(qs)), [None] * len(qs)
+def work(i):
+    with torch.cuda.stream(torch.cuda.Stream()):
+        gate.wait()
+        outs[i] = [fv.fvar_attention_kv4(qs[i], kv, 515) for _ in range(20)]
+threads = [threading.Thread(target=work, args=(i,)) for i in range(len(qs))]
+[t.start() for t in threads], [t.join() for t in threads]
+torch.cuda.synchronize()
+for q, several in zip(qs, outs):
+    alone = fv.fvar_attention_kv4(q, kv, 515)
+    assert all(torch.equal(o, alone) for o in several)
+assert fv.kernel_poll_status() == fv.OK
+print("same")
+"""
+
+
+def test_first_calls_from_several_threads():
+    """A fresh process, whose first calls of every form come at once, each on a stream of its own: each gives what it gives alone."""
+    p = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert p.returncode == 0 and p.stdout == "same\n", (p.stdout, p.stderr[-3000:])
