@@ -285,7 +285,8 @@ fvar_status fvar_poll_status(fvar_ctx *ctx);
 /* Empties the KV cache and the group caches (host state only; device memory is not cleared). */
 fvar_status fvar_reset(fvar_ctx *ctx);
 void fvar_destroy(fvar_ctx *ctx);
-/* Message of the last error on this context (or of the last failed fvar_init when ctx is NULL). */
+/* Message of the last error on this context; with ctx == NULL of the calling thread's last fvar_init or kernel-level call
+ * that failed. */
 const char *fvar_last_error(const fvar_ctx *ctx);
 
 /* ---------------------------------------------------------------------------------------------

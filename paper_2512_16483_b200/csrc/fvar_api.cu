@@ -101,7 +101,8 @@ bool tmap_queries(CUtensorMap *m, const Kv4AttnArgs &a, uint32_t rows) {
 
 __device__ unsigned g_kernel_status;
 
-static std::string g_init_error;
+// Message of the thread's last call that failed without a context: calls come from several threads at once.
+static thread_local std::string g_init_error;
 
 // Address of the status word on the current device (resolved once per device ordinal).
 static unsigned *kernel_status_ptr() {

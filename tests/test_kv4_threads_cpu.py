@@ -2,6 +2,7 @@
 import os
 import re
 import subprocess
+import sys
 
 import pytest
 
@@ -50,3 +51,31 @@ def test_nothing_else_is_kept_between_the_calls():
         with open(os.path.join(build.CSRC, name)) as f:
             kept = re.findall(r"^\s+static (?!constexpr|_*assert)([^(;]*);", f.read(), re.M)
         assert all(re.match(r"PerDevice \w+$|int resident\[kMaxDevices\]", k) for k in kept), (name, kept)
+
+
+ERRORS = """
+import threading
+from paper_2512_16483_b200 import binding as fv
+import ctypes as ct
+lib, P = fv.load_library(), 4096
+cache = ct.byref(fv._Kv4(P, P, P, P, 2, 4, 64, 40, 0))
+calls = {b"kv4: rows outside the cache": lambda: lib.fvar_kv4_read(cache, 3, 39, None, None, P, P, None),
+         b"attention_kv4: bad arguments": lambda: lib.fvar_attention_kv4(P, 512, cache, 8, 0, 40, None, P, None, 0, None),
+         b"kv4_write: K and V must be 16-byte aligned": lambda: lib.fvar_kv4_write(cache, P + 8, P, 256, 3, 0, None, None, None),
+         b"kv4: NULL cache or array": lambda: lib.fvar_kv4_read(None, 3, 39, None, None, P, P, None)}
+wrong, gate = [], threading.Barrier(len(calls))
+def work(text, call):
+    gate.wait()
+    for _ in range(20000):
+        if call() != fv.EINVAL or lib.fvar_last_error(None) != text:
+            wrong.append(text)
+threads = [threading.Thread(target=work, args=x) for x in calls.items()]
+[t.start() for t in threads], [t.join() for t in threads]
+print(len(wrong))
+"""
+
+
+def test_each_thread_has_the_error_of_its_own_call():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    p = subprocess.run([sys.executable, "-c", ERRORS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert p.returncode == 0 and p.stdout == "0\n", (p.returncode, p.stdout, p.stderr[-2000:])
