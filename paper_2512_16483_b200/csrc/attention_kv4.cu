@@ -20,7 +20,6 @@
 // One row of 37 x 8 heads over 10521 keys, D = 128 (424 MB): 82.5 us, 5.1 TB/s; 280 instructions for 16 keys, of which 156 on the ALU
 // pipe (66 % busy, issue slots 59 %, tensor pipe 37 %).  4 rows of 64 x 8 heads over 0 - 8191 keys: 75.6 us, 3.8 TB/s.  One row of 2 x 16
 // heads (46 MB): 17.3 us; 16 rows of 4 x 16 heads over 6441 keys: 26.1.
-#include <float.h>
 #include <limits.h>
 #include <math.h>
 
@@ -256,8 +255,10 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
       const float xt = __bfloat162float(__float2bfloat16_rn(x)), yt = __bfloat162float(__float2bfloat16_rn(y));
       const int term = NG == 4 ? tig >> 1 : tig;
       sums[nb] = term == 0 ? pack_bf2(x, y) : term == 1 ? pack_bf2(x - xt, y - yt) : 0u;
-      // 2^133 for the codes, 2^-sh for the queries; a row with an infinity or a NaN is NaN
-      const float f = e == 255 ? __uint_as_float(0x7FC00000u) : fminf(p.scale_log2 * (k2p66 / f1) * ((2.f * k2p66) / f2), FLT_MAX);
+      // 2^133 for the codes, 2^-sh for the queries; a row with an infinity or a NaN is NaN.  What it multiplies is below 2^11.5 (23 x 128 terms of
+      // 2^-12 and a scale of 3840), so up to 2^116 a score is finite; in a row that would need more (queries from 2^106 on)
+      // the weights are 0 and 1 all the same, unless two scores agree to 2^-120 of the greatest possible.
+      const float f = e == 255 ? __uint_as_float(0x7FC00000u) : fminf(p.scale_log2 * (k2p66 / f1) * ((2.f * k2p66) / f2), 0x1p116f);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         c[nb][i] = __shfl_sync(0xffffffffu, f, (2 * tig + i) * 4);
@@ -455,8 +456,7 @@ attention_kv4_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
   auto store = [&](int row, int d, const float4 &even, const float4 &odd, float l_all) {
     const int rho = rho0 + row;
     if (rho >= nrows || abort_flag != 0) return;
-    // no weight at all: the row sees no key, or its scores are all minus infinity
-    const float inv = l_all != 0.f ? 1.0f / l_all : limit_of(rho) > 0 ? __uint_as_float(0x7FC00000u) : 0.f;
+    const float inv = l_all == 0.f ? 0.f : 1.0f / l_all;  // no weight at all: the row sees no key, since scores are finite or NaN
     *reinterpret_cast<uint4 *>(p.out + ((static_cast<long long>(b) * p.r + rho / G) * p.H + kv * G + rho % G) * D + d) =
         make_uint4(pack_bf2(even.x * inv, odd.x * inv), pack_bf2(even.y * inv, odd.y * inv), pack_bf2(even.z * inv, odd.z * inv), pack_bf2(even.w * inv, odd.w * inv));
   };

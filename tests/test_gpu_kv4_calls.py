@@ -74,6 +74,33 @@ def test_a_row_whose_scores_are_all_minus_infinity_is_nan(fv, r, L, D):
     assert bool(nan[r - 1, 1]) or np.all((far >= seen.min(0) - off) & (far <= seen.max(0) + off))
 
 
+@pytest.mark.parametrize("r,L", [c for c in LAUNCHES if c[0] <= 12])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power", [100, 112, 125])
+def test_few_rows_of_the_largest_queries(fv, r, L, D, power):
+    """Queries up to the end of bf16: one weight is 1, the others are 0, also where a product in fp32 would be infinite.  Keys with the greatest
+    scales and the least ones.  Rows whose two greatest scores are within 2^-9 of the greatest sum of magnitudes are left out: twice what a score
+    may be off by, 2^-14 of 16 / 7 x such a sum for the sums of queries and (D + 8) 2^-23 of it for the rest."""
+    B, H = 2, 2
+    rng = np.random.default_rng(r + L + power)
+    keys = rng.standard_normal((B, H, L, D)) * np.where(np.arange(L) % 2, 8000.0, 2.0 ** -19)[:, None]
+    kv, K, V = _stored(fv, keys, rng.standard_normal((B, H, L, D)))
+    q = si.round_to_bf16((np.clip(rng.standard_normal((B, r, H * D)), -3, 3) * 2.0 ** power).astype(np.float32))
+    got = bf16_to_numpy(fv.fvar_attention_kv4(to_bf16_cuda(q), kv, L)).reshape(B, r, H, D)
+    assert fv.kernel_poll_status() == fv.OK and np.isfinite(got).all()
+    looked = 0
+    for b in range(B):
+        for h in range(H):
+            x = q[b, :, h * D : (h + 1) * D].astype(np.float64)
+            s, far = x @ K[b, h].T, (np.abs(x) @ np.abs(K[b, h]).T).max(-1)
+            best = np.sort(s, -1)
+            for i in np.nonzero(best[:, -1] - best[:, -2] > 2.0 ** -9 * far)[0]:
+                want = V[b, h, s[i].argmax()]
+                assert np.all(np.abs(got[b, i, h] - want) <= 2.0 ** -7 * np.abs(want))        # the weight and the result, a rounding each at most
+                looked += 1
+    assert looked >= B * H * r // 2
+
+
 @pytest.mark.parametrize("native", [True, False])
 def test_attention_where_memory_for_a_workspace_is_short_or_declined(fv, monkeypatch, native):
     """98 MB of workspace that the allocator may not take, or is not asked for: the call runs as the library does without one."""
