@@ -176,3 +176,42 @@ def test_first_calls_from_several_threads():
     """A fresh process, whose first calls of every form come at once, each on a stream of its own: each gives what it gives alone."""
     p = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert p.returncode == 0 and p.stdout == "same\n", (p.stdout, p.stderr[-3000:])
+
+
+FIRST_CALLS_CAPTURED = """
+import torch
+from paper_2512_16483_b200 import binding as fv
+torch.manual_seed(0)
+D, H, L = %d, 2, 515
+rows = torch.randn(1, L, H * D, device="cuda").bfloat16()
+kv, at, lim = fv.Kv4.empty(1, H, 520, D), torch.tensor([3], dtype=torch.int32, device="cuda"), None
+qs = [torch.randn(1, r, H * D, device="cuda").bfloat16() for r in (1, 12, 70, 300, 19000)]
+back = tuple(torch.zeros_like(rows) for _ in range(2))
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    fv.fvar_kv4_write(kv, rows, rows, at)
+    fv.fvar_kv4_read(kv, L, at, out=back)
+    outs = [fv.fvar_attention_kv4(q, kv, L + 3) for q in qs]
+for _ in range(2):
+    rows.normal_()
+    for t in (kv.k_codes, kv.v_codes, kv.k_scales, kv.v_scales):
+        t.zero_()
+    graph.replay()
+    eager = fv.Kv4.empty(1, H, 520, D)
+    for t in (eager.k_codes, eager.v_codes, eager.k_scales, eager.v_scales):
+        t.zero_()
+    fv.fvar_kv4_write(eager, rows, rows, 3)
+    assert torch.equal(fv.fvar_kv4_read(eager, L, 3)[1], back[1])
+    for q, o in zip(qs, outs):
+        assert torch.equal(fv.fvar_attention_kv4(q, eager, L + 3), o)
+assert fv.kernel_poll_status() == fv.OK
+print("same")
+"""
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_first_calls_are_captured(D):
+    """A fresh process whose first calls of every form come inside a capture: nothing that they set up belongs to a stream."""
+    p = subprocess.run([sys.executable, "-c", FIRST_CALLS_CAPTURED % D], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert p.returncode == 0 and p.stdout == "same\n", (p.stdout, p.stderr[-3000:])
