@@ -17,9 +17,9 @@
 //   u - 8           - 8 scale (sum of the group's queries) is a small product of its own, scales x sums in two bf16 terms, and what the
 //                   scores begin with; 8 (sum of a group's P) is one more row of the second product, taken off at the end.
 // ldmatrix gives a key's group as a row (K) and, transposed, pairs of keys in a register (V), so nothing is shuffled.
-// One row of 37 x 8 heads over 10521 keys, D = 128 (424 MB): 82.5 us, 5.1 TB/s; 280 instructions for 16 keys, of which 156 on the ALU
-// pipe (66 % busy, issue slots 59 %, tensor pipe 37 %).  4 rows of 64 x 8 heads over 0 - 8191 keys: 75.6 us, 3.8 TB/s.  One row of 2 x 16
-// heads (46 MB): 17.3 us; 16 rows of 4 x 16 heads over 6441 keys: 26.1.
+// One row of 37 x 8 heads over 10521 keys, D = 128 (424 MB): 82.3 us, 5.1 TB/s; 280 instructions for 16 keys, of which 156 on the ALU
+// pipe (66 % busy, issue slots 59 %, tensor pipe 37 %).  4 rows of 64 x 8 heads over 0 - 8191 keys: 75.7 us, 3.8 TB/s.  One row of 2 x 16
+// heads (46 MB): 17.2 us; 16 rows of 4 x 16 heads over 6441 keys: 26.1.
 #include <limits.h>
 #include <math.h>
 
@@ -554,7 +554,7 @@ static double waves_of(double ctas, double slots, double few) {
 
 // Form, tiles and key ranges of a launch: the least estimated time (microseconds).  The estimates are fitted to forced launches on B200,
 // 10 shapes of few rows and 24 of many, 1 to 5000 rows over 77 to 10521 keys: what they pick of the forms of many rows is 1 % slower than the
-// fastest on average and 7 % at worst.  Few rows: a block costs 5.5 and its keys 7.5 ns each at D = 128 with two blocks an SM, 4.1 with one (0.6 of that at D = 64);
+// fastest on average and 7 % at worst (profiles/kv4_launch_forms.md).  Every element is taken to be L long, also where limits say less.  Few rows: a block costs 5.5 and its keys 7.5 ns each at D = 128 with two blocks an SM, 4.1 with one (0.6 of that at D = 64);
 // 9 to 16 rows at a time, one block an SM, 6.1.  Many rows: see attention_kv4_many_cost.  Where both can be taken they cross between 17 rows
 // (8 units: 11.5 us against 21.8) and 64 (32 units over 8000 keys: 52 against 29).
 Kv4Plan attention_kv4_plan(int B, int Hkv, int G, int r, int D, int L, int num_sms, const int *max_clusters) {

@@ -19,8 +19,8 @@
 // own decodes the cache once into the caller's workspace, and the units (CODES false) request bf16 tiles by TMA.
 //
 // What bounds it is the issue of softmax and decoding together (410 rows of 2 x 16 heads over 2931 keys, D = 128: 35.3 us, 23 blocks of 1.3 us
-// in 128 CTAs, tensor pipe 36 %, issue slots 39 % busy), at the largest size also the clock under load (4096 rows over 10521 keys: 594 us,
-// 36 of them the pass, 1.19 PFLOP/s, in a short run, 680 to 690 in a long one).
+// in 128 CTAs, tensor pipe 36 %, issue slots 39 % busy), at the largest size also the clock under load (4096 rows over 10521 keys: 570 to 580 us,
+// 36 of them the pass, 1.22 PFLOP/s, in a short run, 690 to 705 in a long one).
 #include <limits.h>
 #include <math.h>
 

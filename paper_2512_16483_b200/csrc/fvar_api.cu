@@ -76,7 +76,6 @@ bool tmap_kblocks(CUtensorMap *m, const void *base, uint64_t rows, uint64_t kblo
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Status word used by the kernel-level entry points (contexts carry their own in the workspace).
 bool tmap_codes(CUtensorMap *m, const void *codes, const Kv4AttnArgs &a, uint32_t rows) {
   if (!tmap_init_driver()) return false;
   const cuuint64_t row = a.D / 2;
@@ -99,6 +98,7 @@ bool tmap_queries(CUtensorMap *m, const Kv4AttnArgs &a, uint32_t rows) {
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Status word used by the kernel-level entry points (contexts carry their own in the workspace).
 __device__ unsigned g_kernel_status;
 
 // Message of the thread's last call that failed without a context: calls come from several threads at once.
