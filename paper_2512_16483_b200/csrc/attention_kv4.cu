@@ -554,7 +554,8 @@ static double waves_of(double ctas, double slots, double few) {
 
 // Form, tiles and key ranges of a launch: the least estimated time (microseconds).  The estimates are fitted to forced launches on B200,
 // 10 shapes of few rows and 24 of many, 1 to 5000 rows over 77 to 10521 keys: what they pick of the forms of many rows is 1 % slower than the
-// fastest on average and 7 % at worst (profiles/kv4_launch_forms.md).  Every element is taken to be L long, also where limits say less.  Few rows: a block costs 5.5 and its keys 7.5 ns each at D = 128 with two blocks an SM, 4.1 with one (0.6 of that at D = 64);
+// fastest on average and 7 % at worst.  Every element is taken to be L long, also where limits say less.
+// Few rows: a block costs 5.5 and its keys 7.5 ns each at D = 128 with two blocks an SM, 4.1 with one (0.6 of that at D = 64);
 // 9 to 16 rows at a time, one block an SM, 6.1.  Many rows: see attention_kv4_many_cost.  Where both can be taken they cross between 17 rows
 // (8 units: 11.5 us against 21.8) and 64 (32 units over 8000 keys: 52 against 29).
 Kv4Plan attention_kv4_plan(int B, int Hkv, int G, int r, int D, int L, int num_sms, const int *max_clusters) {
